@@ -323,6 +323,102 @@ int topk_set_workspace(void* dev_ptr, size_t bytes);
 #define TOPK_SHORT_ROW_KERNEL_GENERAL 2
 int topk_set_route(int which, int value);
 
+/*
+ * ---- Behind a router -------------------------------------------------------------------------------------------------
+ *
+ * The path of a sparse mixture of experts behind its router (Sec. 6): experts are chosen per token, by topk_mask_sparse_fwd
+ * (relaxed) or topk_route_fwd (hard); topk_expert_map gives every chosen (token, choice) pair its place in expert order;
+ * topk_expert_product_* multiplies every expert's rows by its matrix; topk_combine_* adds the experts' rows up per token.
+ * Each has its vector-Jacobian product.
+ *   - Values come as TOPK_TYPE_*; sums, statistics, weights (val) and their gradients are float32 or wider, every output is
+ *     rounded once.  Strides are in elements, >= 0 (0: one row for all); outputs are contiguous unless said otherwise.
+ *   - The calls use no registered workspace: they may overlap on several streams and in several captured graphs.
+ *   - Indices and places are checked on the device: what is out of range counts as an empty place, nothing out of range is
+ *     read or written.
+ */
+enum { TOPK_TYPE_F32 = 0, TOPK_TYPE_BF16 = 1, TOPK_TYPE_F16 = 2 };
+enum { TOPK_SCORE_SOFTMAX = 0, TOPK_SCORE_SIGMOID = 1 };
+#define TOPK_EXPERTS_MAX 1024       /* experts */
+#define TOPK_CHOICES_MAX 64         /* choices per token of topk_route_* */
+#define TOPK_ROUTE_GROUPS_MAX 64    /* groups of experts of topk_route_fwd */
+
+/*
+ * Hard routing.  Per row of logits l: s = softmax(l) or 1 / (1 + exp(-l)); c = s + bias.  The k largest c in descending
+ * order (ties: ascending index) give idx_out, val_out = scale * s at them, divided by their sum with `renormalise`.  The
+ * bias (may be NULL) moves the choice only, e.g. towards a balanced load; without it the order is that of the logits.
+ * groups > 1: experts lie in `groups` equal consecutive groups, and only the keep_groups groups of the largest score are
+ * chosen from (ties: the lower group), the score being the largest c of the group (group_top = 1) or the sum of its two
+ * largest (group_top = 2).  Scores are compared in float64.
+ *   A logit of -inf or NaN, or a bias of -inf or NaN, takes its expert out of the choice (the logit also out of the softmax).
+ *   Where fewer than k experts are left the remaining places hold -1 / 0.0f: a row of -inf (a padded token) is all empty.
+ *   logits [rows][n] of `type`, `stride` elements between rows; bias [n] float or NULL; idx_out (int32), val_out (float)
+ *   [rows][k].  1 <= n <= TOPK_EXPERTS_MAX, 1 <= k <= min(TOPK_CHOICES_MAX, n / groups * keep_groups), groups divides n.
+ */
+int topk_route_fwd(const void* logits, int type, int64_t stride, const float* bias, int64_t rows, int64_t n, int64_t k,
+                   int score, int64_t groups, int64_t keep_groups, int group_top, int renormalise, double scale,
+                   int32_t* idx_out, float* val_out, void* stream);
+
+/*
+ * Its vector-Jacobian product in the logits, for the experts chosen: grad_out = d <val, cotangent> / d logits, val as
+ * above at the given idx (neither the choice nor the bias has a gradient).  Empty places carry none.
+ *   idx, cotangent [rows][k]; grad_out [rows][n] of the logits' type.
+ */
+int topk_route_vjp(const void* logits, int type, int64_t stride, const int32_t* idx, const float* cotangent, int64_t rows,
+                   int64_t n, int64_t k, int score, int renormalise, double scale, void* grad_out, void* stream);
+
+/*
+ * Places of the pairs (t, j) of idx [rows][k] in expert order: expert by expert, within an expert by ascending t * k + j.
+ *   load_out [n]: pairs that chose the expert.  Of these the first `capacity` are kept (0: all).
+ *   offset_out [n + 1]: expert e has the places offset[e] .. offset[e + 1] - 1.
+ *   slot_out [rows][k]: place of the pair, -1 where idx is out of [0, n) or the expert is full.
+ *   source_out [rows * k]: the pair t * k + j behind a place, -1 from offset[n] on.
+ *   rows * k < 2^31.  scratch: topk_expert_map_bytes(rows, k, n) bytes of the caller's for this call (TOPK_ERR_WORKSPACE if
+ *   smaller), 4-byte aligned; calls that may overlap need one each.
+ */
+size_t topk_expert_map_bytes(int64_t rows, int64_t k, int64_t n);
+int topk_expert_map(const int32_t* idx, int64_t rows, int64_t k, int64_t n, int64_t capacity, int32_t* slot_out,
+                    int32_t* source_out, int32_t* offset_out, int32_t* load_out, void* scratch, size_t scratch_bytes,
+                    void* stream);
+
+/*
+ * The experts' products.  For every place s of expert e: out[s] = W[e] x[r(s)], r(s) = source[s] / k, or s where source is
+ * NULL (rows of x in expert order).  Rows of out behind offset[n] are left as they were.
+ *   x [m][h] of `type`, x_stride between rows; w(e, o, i) at w[e * w_expert + o * w_out + i * w_in], o < ho, i < h, w_out or
+ *   w_in being 1; offset [n + 1] non-decreasing from 0 to at most slots; source [slots] or NULL; out [slots][ho].
+ *   A place whose source is out of range has a row of zeros.
+ */
+int topk_expert_product_fwd(const void* x, int64_t x_stride, int64_t m, const void* w, int64_t w_expert, int64_t w_out,
+                            int64_t w_in, const int32_t* offset, const int32_t* source, int64_t k, int64_t slots, int64_t n,
+                            int64_t h, int64_t ho, int type, void* out, void* stream);
+
+/*
+ * Its gradients (either output may be NULL):  dx_out[s] = W[e]^T cotangent[s], per PLACE, rows behind offset[n] left as they
+ * were (with source, topk_combine_fwd(dx_out, slot, NULL, ..) sums them to the rows of x);
+ * dW_out[e] = sum over e's places of cotangent[s] x[r(s)]^T, zeros for an expert without places.
+ *   cotangent [slots][ho]; dx_out [slots][h]; dw_out [n][ho][h] contiguous where w_in is 1, otherwise [n][h][ho].
+ */
+int topk_expert_product_vjp(const void* x, int64_t x_stride, int64_t m, const void* w, int64_t w_expert, int64_t w_out,
+                            int64_t w_in, const int32_t* offset, const int32_t* source, int64_t k, int64_t slots, int64_t n,
+                            int64_t h, int64_t ho, int type, const void* cotangent, int64_t cotangent_stride, void* dx_out,
+                            void* dw_out, void* stream);
+
+/*
+ * Weighted sum per token: out[t] = sum_j val[t][j] y[slot[t][j]] (val NULL: ones), places out of [0, slots) left out.
+ *   y [slots][h] of `type`, y_stride between rows; slot, val [rows][k]; out [rows][h].
+ */
+int topk_combine_fwd(const void* y, int64_t y_stride, const int32_t* slot, const float* val, int64_t rows, int64_t k,
+                     int64_t slots, int64_t h, int type, void* out, void* stream);
+
+/*
+ * Its gradients: dy_out[slot[t][j]] = val[t][j] cotangent[t], rows that no pair names left as they were;
+ * dval_out[t][j] = <cotangent[t], y[slot[t][j]]>, 0 for an empty place (NULL with val NULL: not wanted; y may be NULL then).
+ * A place is named by one pair at most, as topk_expert_map gives them (where two name it, dy_out there is one of theirs).
+ *   cotangent [rows][h]; dy_out [slots][h] contiguous; dval_out [rows][k].
+ */
+int topk_combine_vjp(const void* y, int64_t y_stride, const int32_t* slot, const float* val, const void* cotangent,
+                     int64_t cotangent_stride, int64_t rows, int64_t k, int64_t slots, int64_t h, int type, void* dy_out,
+                     float* dval_out, void* stream);
+
 /* Static, human-readable text for a return code. */
 const char* topk_strerror(int code);
 

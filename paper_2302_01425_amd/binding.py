@@ -25,6 +25,8 @@ EXPORTS = (
     "topk_mask_sparse_fwd", "topk_general_fwd", "topk_general_jvp", "topk_mask_dykstra_fwd", "topk_signed_mask_fwd", "topk_signed_mask_jvp", "topk_masked_value_fwd", "topk_masked_value_jvp",
     "topk_mask_loss", "topk_argsort_desc", "topk_workspace_bytes", "topk_set_workspace",
     "topk_set_route", "topk_strerror", "topk_mask_jvp_static",
+    "topk_route_fwd", "topk_route_vjp", "topk_expert_map", "topk_expert_map_bytes", "topk_expert_product_fwd",
+    "topk_expert_product_vjp", "topk_combine_fwd", "topk_combine_vjp",
 )
 
 _lib = None
@@ -72,6 +74,19 @@ def load() -> ctypes.CDLL:
     L.topk_mask_loss.restype = ci
     for name in ("topk_mask_fwd", "topk_mask_jvp", "topk_mask_vjp", "topkmag_fwd", "topkmag_jvp",
                  "topkmag_vjp", "topk_argsort_desc"):
+        getattr(L, name).restype = ci
+    L.topk_route_fwd.argtypes = [vp, ci, i64, vp, i64, i64, i64, ci, i64, i64, ci, ci, dbl, vp, vp, vp]
+    L.topk_route_vjp.argtypes = [vp, ci, i64, vp, vp, i64, i64, i64, ci, ci, dbl, vp, vp]
+    L.topk_expert_map.argtypes = [vp, i64, i64, i64, i64, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    L.topk_expert_map_bytes.argtypes = [i64, i64, i64]
+    L.topk_expert_map_bytes.restype = ctypes.c_size_t
+    product = [vp, i64, i64, vp, i64, i64, i64, vp, vp, i64, i64, i64, i64, i64, ci]
+    L.topk_expert_product_fwd.argtypes = product + [vp, vp]
+    L.topk_expert_product_vjp.argtypes = product + [vp, i64, vp, vp, vp]
+    L.topk_combine_fwd.argtypes = [vp, i64, vp, vp, i64, i64, i64, i64, ci, vp, vp]
+    L.topk_combine_vjp.argtypes = [vp, i64, vp, vp, vp, i64, i64, i64, i64, i64, ci, vp, vp, vp]
+    for name in ("topk_route_fwd", "topk_route_vjp", "topk_expert_map", "topk_expert_product_fwd",
+                 "topk_expert_product_vjp", "topk_combine_fwd", "topk_combine_vjp"):
         getattr(L, name).restype = ci
     L.topk_workspace_bytes.argtypes = [ci, i64, i64, i64, dbl]
     L.topk_workspace_bytes.restype = ctypes.c_size_t
@@ -552,3 +567,269 @@ def topk_argsort_desc(theta, perm_out=None, stream=None):
     _enqueue("topk_argsort_desc", TOPK_OP_ARGSORT, rows, n, 0, 2.0, theta,
              theta.data_ptr(), rows, n, perm_out.data_ptr(), _stream(stream))
     return perm_out
+
+
+# ---- behind a router: choosing experts, places, the experts' products, the sum per token --------------------------------
+# These take float32, bfloat16 and float16, rows at any stride, and tensors of any device: the work goes to the given
+# stream, by default the current one of the tensors' device.  Outputs that are not passed in are allocated for that stream.
+TOPK_SCORE_SOFTMAX, TOPK_SCORE_SIGMOID = 0, 1
+TOPK_EXPERTS_MAX, TOPK_CHOICES_MAX, TOPK_ROUTE_GROUPS_MAX = 1024, 64, 64
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _on(ref: torch.Tensor, stream, call):
+    """call(raw stream) with the device of `ref` current, and the stream, so that what it allocates belongs to it."""
+    index = ref.get_device()
+    if stream is None and torch.cuda.current_device() == index:
+        return call(_stream(None))
+    with torch.cuda.device(index):
+        if stream is None:
+            return call(_stream(None))
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(_stream(stream), device=index)
+        elif stream.device_index != index:
+            raise TopkError(f"stream belongs to {stream.device}, the tensors to {ref.device}")
+        with torch.cuda.stream(stream):
+            return call(int(stream.cuda_stream))
+
+
+def _rows(t, name: str, ref: torch.Tensor | None = None, dtype=None) -> torch.Tensor:
+    """A 2-D tensor of values with contiguous rows, of the type and on the device of `ref`."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TopkError(f"{name} must be a tensor in GPU memory")
+    if t.dim() != 2 or t.dtype not in _TYPES or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise TopkError(f"{name} must be a 2-D float32, bfloat16 or float16 tensor with contiguous rows")
+    if ref is not None and (t.dtype != ref.dtype or t.get_device() != ref.get_device()):
+        raise TopkError(f"{name} must be of type {ref.dtype} on {ref.device} (got {t.dtype} on {t.device})")
+    return t
+
+
+def _exact(t, shape, dtype, ref: torch.Tensor, name: str) -> torch.Tensor:
+    """A contiguous tensor of this shape and type on the device of `ref`."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or tuple(t.shape) != tuple(shape) or \
+            t.get_device() != ref.get_device() or not t.is_contiguous():
+        raise TopkError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {ref.device}")
+    return t
+
+
+def _reach(t: torch.Tensor):
+    """First byte and the one behind the last that the tensor reaches."""
+    start = t.data_ptr()
+    if t.numel() == 0:
+        return start, start
+    return start, start + (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1) * t.element_size()
+
+
+def _apart(outs, inputs) -> None:
+    """Outputs that were passed in (name, tensor) overlap neither an input nor each other."""
+    seen = [(_reach(t), "an input tensor (outputs must not alias inputs)") for t in inputs if t is not None]
+    for name, t in outs:
+        if t is None:
+            continue
+        a, b = _reach(t)
+        for (c, d), what in seen:
+            if a < d and c < b:
+                raise TopkError(f"{name} overlaps {what}")
+        seen.append(((a, b), name))
+
+
+def _new(t, shape, dtype, ref):
+    return torch.empty(shape, dtype=dtype, device=ref.device) if t is None else t
+
+
+def topk_route_fwd(logits, k, score=TOPK_SCORE_SOFTMAX, bias=None, groups=1, keep_groups=1, group_top=1,
+                   renormalise=True, scale=1.0, idx_out=None, val_out=None, stream=None):
+    """Returns (idx [rows, k] int32, val [rows, k] float32)."""
+    logits = _rows(logits, "logits")
+    rows, n = logits.shape
+    k = int(k)
+    if bias is not None:
+        _exact(bias, (n,), _F32, logits, "bias")
+    if idx_out is not None or val_out is not None:
+        for t, dtype, name in ((idx_out, torch.int32, "idx_out"), (val_out, _F32, "val_out")):
+            if t is not None:
+                _exact(t, (rows, k), dtype, logits, name)
+        _apart((("idx_out", idx_out), ("val_out", val_out)), (logits, bias))
+
+    def call(st):
+        if k < 0:
+            _check(-1, "topk_route_fwd")
+        idx = _new(idx_out, (rows, k), torch.int32, logits)
+        val = _new(val_out, (rows, k), _F32, logits)
+        _check((_lib or load()).topk_route_fwd(
+            logits.data_ptr(), _TYPES[logits.dtype], logits.stride(0), None if bias is None else bias.data_ptr(), rows, n, k,
+            int(score), int(groups), int(keep_groups), int(group_top), int(bool(renormalise)), float(scale), idx.data_ptr(),
+            val.data_ptr(), st), "topk_route_fwd")
+        return idx, val
+    return _on(logits, stream, call)
+
+
+def topk_route_vjp(logits, idx, cotangent, score=TOPK_SCORE_SOFTMAX, renormalise=True, scale=1.0, grad_out=None,
+                   stream=None):
+    """Returns the gradient in the logits, [rows, n] of their type, of the weights at the chosen idx [rows, k]."""
+    logits = _rows(logits, "logits")
+    rows, n = logits.shape
+    if not isinstance(idx, torch.Tensor) or idx.dim() != 2:
+        raise TopkError("idx must be a 2-D int32 tensor [rows, k]")
+    k = idx.shape[1]
+    _exact(idx, (rows, k), torch.int32, logits, "idx")
+    _exact(cotangent, (rows, k), _F32, logits, "cotangent")
+    if grad_out is not None:
+        _exact(grad_out, (rows, n), logits.dtype, logits, "grad_out")
+        _apart((("grad_out", grad_out),), (logits, idx, cotangent))
+
+    def call(st):
+        grad = _new(grad_out, (rows, n), logits.dtype, logits)
+        _check((_lib or load()).topk_route_vjp(
+            logits.data_ptr(), _TYPES[logits.dtype], logits.stride(0), idx.data_ptr(), cotangent.data_ptr(), rows, n, k,
+            int(score), int(bool(renormalise)), float(scale), grad.data_ptr(), st), "topk_route_vjp")
+        return grad
+    return _on(logits, stream, call)
+
+
+def topk_expert_map(idx, n, capacity=0, slot_out=None, source_out=None, offset_out=None, load_out=None, stream=None):
+    """Returns (slot [rows, k], source [rows * k], offset [n + 1], load [n]), int32, for the chosen experts idx [rows, k]."""
+    if not isinstance(idx, torch.Tensor) or not idx.is_cuda or idx.dim() != 2:
+        raise TopkError("idx must be a 2-D int32 tensor [rows, k] in GPU memory")
+    rows, k = idx.shape
+    n = int(n)
+    _exact(idx, (rows, k), torch.int32, idx, "idx")
+    if not 1 <= n <= TOPK_EXPERTS_MAX:
+        _check(-1, "topk_expert_map")
+    shapes = ((rows, k), (rows * k,), (n + 1,), (n,))
+    given = (("slot_out", slot_out), ("source_out", source_out), ("offset_out", offset_out), ("load_out", load_out))
+    if any(t is not None for _, t in given):
+        for (name, t), shape in zip(given, shapes):
+            if t is not None:
+                _exact(t, shape, torch.int32, idx, name)
+        _apart(given, (idx,))
+
+    def call(st):
+        L = _lib or load()
+        outs = [_new(t, shape, torch.int32, idx) for (_, t), shape in zip(given, shapes)]
+        need = L.topk_expert_map_bytes(rows, k, n)
+        scratch = torch.empty(need, dtype=torch.uint8, device=idx.device) if need else None
+        _check(L.topk_expert_map(idx.data_ptr(), rows, k, n, int(capacity), *(t.data_ptr() for t in outs),
+                                 None if scratch is None else scratch.data_ptr(), need, st), "topk_expert_map")
+        return tuple(outs)
+    return _on(idx, stream, call)
+
+
+def _product(x, w, offset, source, k):
+    """Checked arguments of the experts' products: what the library takes of x, w and the lists, and the shapes."""
+    x = _rows(x, "x")
+    if not isinstance(w, torch.Tensor) or w.dim() != 3 or w.dtype != x.dtype or w.get_device() != x.get_device() or \
+            w.shape[2] != x.shape[1]:
+        raise TopkError(f"w must be a {x.dtype} tensor [n, out, {x.shape[1]}] on {x.device}")
+    n, ho, h = w.shape
+    w_expert, w_out, w_in = w.stride()
+    if h == 1:
+        w_in = 1
+    elif ho == 1 and w_in != 1:
+        w_out = 1
+    if w_in != 1 and w_out != 1:
+        raise TopkError("w must be contiguous along its last dimension or the one before it")
+    _exact(offset, (n + 1,), torch.int32, x, "offset")
+    slots = x.shape[0]
+    if source is not None:
+        if not isinstance(source, torch.Tensor) or source.dim() != 1:
+            raise TopkError("source must be a 1-D int32 tensor")
+        slots = source.shape[0]
+        _exact(source, (slots,), torch.int32, x, "source")
+    args = (x.data_ptr(), x.stride(0), x.shape[0], w.data_ptr(), w_expert, w_out, w_in, offset.data_ptr(),
+            None if source is None else source.data_ptr(), int(k), slots, n, h, ho, _TYPES[x.dtype])
+    return x, slots, n, h, ho, w_in == 1, args
+
+
+def topk_expert_product_fwd(x, w, offset, source=None, k=1, out=None, stream=None):
+    """Returns out [slots, ho]: W[e] x[source // k] for every place, w [n, ho, h]; without source the rows of x are in expert
+    order.  Rows behind offset[n] are not written."""
+    x, slots, n, h, ho, _, args = _product(x, w, offset, source, k)
+    if out is not None:
+        _exact(out, (slots, ho), x.dtype, x, "out")
+        _apart((("out", out),), (x, w, offset, source))
+
+    def call(st):
+        y = _new(out, (slots, ho), x.dtype, x)
+        _check((_lib or load()).topk_expert_product_fwd(*args, y.data_ptr(), st), "topk_expert_product_fwd")
+        return y
+    return _on(x, stream, call)
+
+
+def topk_expert_product_vjp(x, w, offset, cotangent, source=None, k=1, want_x=True, want_w=True, dx_out=None, dw_out=None,
+                            stream=None):
+    """Returns (dx [slots, h] per place, dw like w); one that is not wanted is None.  Rows of dx behind offset[n] are not
+    written; with source, topk_combine_fwd(dx, slot) gives the gradient of x."""
+    x, slots, n, h, ho, plain, args = _product(x, w, offset, source, k)
+    cotangent = _rows(cotangent, "cotangent", x)
+    if tuple(cotangent.shape) != (slots, ho):
+        raise TopkError(f"cotangent must have the shape {(slots, ho)} (got {tuple(cotangent.shape)})")
+    if dx_out is not None:
+        _exact(dx_out, (slots, h), x.dtype, x, "dx_out")
+    if dw_out is not None:
+        like = dw_out if plain or not isinstance(dw_out, torch.Tensor) or dw_out.dim() != 3 else dw_out.transpose(1, 2)
+        _exact(like, (n, ho, h) if plain else (n, h, ho), x.dtype, x, "dw_out" if plain else "dw_out, transposed like w,")
+    _apart((("dx_out", dx_out), ("dw_out", dw_out)), (x, w, offset, source, cotangent))
+
+    def call(st):
+        dx = _new(dx_out, (slots, h), x.dtype, x) if want_x or dx_out is not None else None
+        dw = dw_out
+        if dw is None and want_w:
+            dw = _new(None, (n, ho, h), x.dtype, x) if plain else _new(None, (n, h, ho), x.dtype, x).transpose(1, 2)
+        if dx is None and dw is None:
+            return None, None
+        _check((_lib or load()).topk_expert_product_vjp(
+            *args, cotangent.data_ptr(), cotangent.stride(0), None if dx is None else dx.data_ptr(),
+            None if dw is None else dw.data_ptr(), st), "topk_expert_product_vjp")
+        return dx, dw
+    return _on(x, stream, call)
+
+
+def _combine(y, slot, val):
+    y = _rows(y, "y")
+    if not isinstance(slot, torch.Tensor) or slot.dim() != 2:
+        raise TopkError("slot must be a 2-D int32 tensor [rows, k]")
+    _exact(slot, slot.shape, torch.int32, y, "slot")
+    if val is not None:
+        _exact(val, slot.shape, _F32, y, "val")
+    return y, slot.shape[0], slot.shape[1], y.shape[0], y.shape[1]
+
+
+def topk_combine_fwd(y, slot, val=None, out=None, stream=None):
+    """Returns out [rows, h]: the sum over j of val[t, j] * y[slot[t, j]] (val None: ones)."""
+    y, rows, k, slots, h = _combine(y, slot, val)
+    if out is not None:
+        _exact(out, (rows, h), y.dtype, y, "out")
+        _apart((("out", out),), (y, slot, val))
+
+    def call(st):
+        o = _new(out, (rows, h), y.dtype, y)
+        _check((_lib or load()).topk_combine_fwd(
+            y.data_ptr(), y.stride(0), slot.data_ptr(), None if val is None else val.data_ptr(), rows, k, slots, h,
+            _TYPES[y.dtype], o.data_ptr(), st), "topk_combine_fwd")
+        return o
+    return _on(y, stream, call)
+
+
+def topk_combine_vjp(y, slot, val, cotangent, dy_out=None, dval_out=None, stream=None):
+    """Returns (dy [slots, h], dval [rows, k]; None with val None).  Rows of dy that no pair names are not written."""
+    y, rows, k, slots, h = _combine(y, slot, val)
+    cotangent = _rows(cotangent, "cotangent", y)
+    if tuple(cotangent.shape) != (rows, h):
+        raise TopkError(f"cotangent must have the shape {(rows, h)} (got {tuple(cotangent.shape)})")
+    if dy_out is not None or dval_out is not None:
+        if dy_out is not None:
+            _exact(dy_out, (slots, h), y.dtype, y, "dy_out")
+        if dval_out is not None:
+            _exact(dval_out, (rows, k), _F32, y, "dval_out")
+        _apart((("dy_out", dy_out), ("dval_out", dval_out)), (y, slot, val, cotangent))
+
+    def call(st):
+        dy = _new(dy_out, (slots, h), y.dtype, y)
+        dval = dval_out if val is None else _new(dval_out, (rows, k), _F32, y)
+        _check((_lib or load()).topk_combine_vjp(
+            y.data_ptr(), y.stride(0), slot.data_ptr(), None if val is None else val.data_ptr(), cotangent.data_ptr(),
+            cotangent.stride(0), rows, k, slots, h, _TYPES[y.dtype], dy.data_ptr(),
+            None if dval is None else dval.data_ptr(), st), "topk_combine_vjp")
+        return dy, dval
+    return _on(y, stream, call)
