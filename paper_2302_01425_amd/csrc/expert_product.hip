@@ -6,32 +6,10 @@
 //   C(m, n) = sum_k A(m, k) B(n, k)
 // with A, B each either contiguous in k or contiguous in m / n, and a row of x found through `source`.  Matrix instructions
 // with float32 sums, one rounding per output element.
-#include "common.hpp"
-#include "experts.hpp"
+#include "expert_product.hpp"
 
 namespace topk {
 namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef f16 f16x8 __attribute__((ext_vector_type(8)));
-
-// 16 x 16 outputs += 64 bytes of k: lane l holds the 16 bytes of k at (l / 16) * 16 of row l % 16 of either operand.
-// (float32 takes four instructions of one k per lane; which k meets which is the same on both sides.)
-__device__ __forceinline__ f32x4 mma(const bf16* a, const bf16* b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(a), *reinterpret_cast<const bf16x8*>(b), c, 0,
-                                                 0, 0);
-}
-__device__ __forceinline__ f32x4 mma(const f16* a, const f16* b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const f16x8*>(a), *reinterpret_cast<const f16x8*>(b), c, 0, 0,
-                                                0);
-}
-__device__ __forceinline__ f32x4 mma(const float* a, const float* b, f32x4 c) {
-  const f32x4 u = *reinterpret_cast<const f32x4*>(a), v = *reinterpret_cast<const f32x4*>(b);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(u[i], v[i], c, 0, 0, 0);
-  return c;
-}
 
 // One operand: element (row, k) at p[row * stride + k] (contiguous in k) or p[k * stride + row]; the index that `stride`
 // belongs to goes through source / div where there is one, and is out where that is not in [0, limit).
@@ -40,69 +18,22 @@ struct Side {
   const T* p;
   int64_t stride;
   const int32_t* source;
-  int64_t div, limit;
+  Divisor div;
+  int64_t limit;
   __device__ __forceinline__ const T* at(int64_t i) const {        // null: out
     if (source != nullptr) {
-      i = source[i];
-      if (i < 0) return nullptr;
-      i /= div;
+      const int pair = source[i];
+      if (pair < 0) return nullptr;
+      i = quotient(pair, div);
     }
     return i < limit ? p + i * stride : nullptr;
   }
 };
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kProductThreads;
 constexpr int kTile = 128;             // rows and columns of a workgroup's outputs
 constexpr int kStep = 64;              // bytes of k per step
 constexpr int kPitch = kStep + 16;     // bytes between rows in LDS
-
-// [begin, end) of expert e, inside [0, slots) whatever the array holds
-__device__ __forceinline__ void places(const int32_t* offset, int e, int64_t slots, int64_t* begin, int64_t* end) {
-  *begin = min(max(int64_t(offset[e]), int64_t(0)), slots);
-  *end = min(max(int64_t(offset[e + 1]), *begin), slots);
-}
-
-// The `tile`-th tile of `size` rows, the experts' rows cut into tiles one expert after the other: its expert and rows, or
-// false behind the last.  All threads of the workgroup call it.
-struct Found {
-  int expert;
-  int64_t begin, end;
-};
-__device__ __forceinline__ bool find_tile(const int32_t* offset, int n, int64_t slots, int64_t tile, int size, Found* f) {
-  __shared__ int64_t wave_total[kThreads / kWave];
-  __shared__ Found found;
-  constexpr int kOwn = kExpertsMax / kThreads;
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-  int64_t b[kOwn], e[kOwn], mine = 0;
-#pragma unroll
-  for (int i = 0; i < kOwn; ++i) {
-    b[i] = e[i] = 0;
-    if (tid * kOwn + i < n) places(offset, tid * kOwn + i, slots, &b[i], &e[i]);
-    mine += (e[i] - b[i] + size - 1) / size;
-  }
-  int64_t scan = mine;
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int64_t v = __shfl_up(scan, off, kWave);
-    if (lane >= off) scan += v;
-  }
-  if (lane == kWave - 1) wave_total[wave] = scan;
-  if (tid == 0) found.expert = -1;
-  __syncthreads();
-  int64_t start = scan - mine;
-  for (int w = 0; w < wave; ++w) start += wave_total[w];
-#pragma unroll
-  for (int i = 0; i < kOwn; ++i) {
-    const int64_t tiles = (e[i] - b[i] + size - 1) / size;
-    if (tile >= start && tile < start + tiles) {
-      const int64_t first = b[i] + (tile - start) * size;
-      found = Found{tid * kOwn + i, first, min(first + size, e[i])};
-    }
-    start += tiles;
-  }
-  __syncthreads();
-  *f = found;
-  return f->expert >= 0;
-}
 
 // 16 bytes per thread and turn of one operand's step (k0 .. k0 + 64 bytes), rows [r0, r0 + 128) up to `rows`, to LDS as
 // [row][k]
@@ -158,10 +89,10 @@ __device__ __forceinline__ void tile_product(const Side<T>& a, const Side<T>& b,
     const int off = (lane & 15) * kPitch + (lane >> 4) * 16;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const T* fa = reinterpret_cast<const T*>(lds_a + (wm + 16 * i) * kPitch + off);
+      const Fragment<T> fa = *reinterpret_cast<const Fragment<T>*>(lds_a + (wm + 16 * i) * kPitch + off);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const T* fb = reinterpret_cast<const T*>(lds_b + (wn + 16 * j) * kPitch + off);
+        const Fragment<T> fb = *reinterpret_cast<const Fragment<T>*>(lds_b + (wn + 16 * j) * kPitch + off);
         acc[i][j] = mma(fb, fa, acc[i][j]);      // (n along the registers of a lane: stores of four neighbours)
       }
     }
@@ -189,43 +120,21 @@ __device__ __forceinline__ void tile_product(const Side<T>& a, const Side<T>& b,
   }
 }
 
-// forward and dx: rows of A are places, B is W[e] seen as [n][k] (contiguous in k or in n)
-struct RowsArgs {
-  const void* a;
-  int64_t a_stride;
-  const int32_t* source;
-  int64_t div, limit;
-  const void* w;
-  int64_t w_expert, w_stride;
-  const int32_t* offset;
-  int64_t slots;
-  int n;
-  int64_t cols, depth, col_tiles;
-  void* c;
-};
 template <class T, bool B_KC>
 __global__ __launch_bounds__(kThreads) void rows_kernel(RowsArgs g) {
   Found f;
-  if (!find_tile(g.offset, g.n, g.slots, blockIdx.x / g.col_tiles, kTile, &f)) return;
+  if (!find_tile(g.offset, g.n, g.slots, blockIdx.x, g.col_tiles, kTile, &f)) return;
   const Side<T> a{static_cast<const T*>(g.a), g.a_stride, g.source, g.div, g.limit};
-  const Side<T> b{static_cast<const T*>(g.w) + f.expert * g.w_expert, g.w_stride, nullptr, 1, INT64_MAX};
-  tile_product<T, true, B_KC>(a, b, f.begin, f.end, int64_t(blockIdx.x % g.col_tiles) * kTile, g.cols, 0, g.depth,
+  const Side<T> b{static_cast<const T*>(g.w) + f.expert * g.w_expert, g.w_stride, nullptr, Divisor{}, INT64_MAX};
+  tile_product<T, true, B_KC>(a, b, f.begin, f.end, f.col * kTile, g.cols, 0, g.depth,
                               static_cast<T*>(g.c), g.cols);
 }
 
-// dW: k runs over an expert's places; one of the two operands goes through `source`
-struct WeightArgs {
-  const void *a, *b;
-  int64_t a_stride, b_stride;
-  const int32_t *a_source, *b_source;
-  int64_t div, a_limit, b_limit;
-  const int32_t* offset;
-  int64_t slots, m, cols, m_tiles, col_tiles;
-  void* c;
-};
 template <class T>
 __global__ __launch_bounds__(kThreads) void weight_kernel(WeightArgs g) {
-  const int64_t col = blockIdx.x % g.col_tiles, rest = blockIdx.x / g.col_tiles;
+  const int64_t tile = die_order(blockIdx.x, g.n * g.m_tiles * g.col_tiles);
+  if (tile < 0) return;
+  const int64_t col = tile % g.col_tiles, rest = tile / g.col_tiles;
   const int e = int(rest / g.m_tiles);
   int64_t begin, end;
   places(g.offset, e, g.slots, &begin, &end);
@@ -241,13 +150,14 @@ template <class T>
 int rows_type(RowsArgs g, bool k_contiguous, hipStream_t stream) {
   g.col_tiles = tiles(g.cols);
   const int64_t most = g.slots / kTile + min(int64_t(g.n), g.slots);       // tiles of rows, at most
-  const int64_t blocks = most * g.col_tiles;
+  const int64_t blocks = most * g.col_tiles + kDies - 1;                   // (the eight runs may end short)
   if (blocks >= (int64_t(1) << 31)) return -1;
   if (k_contiguous) hipLaunchKernelGGL((rows_kernel<T, true>), dim3(unsigned(blocks)), dim3(kThreads), 0, stream, g);
   else hipLaunchKernelGGL((rows_kernel<T, false>), dim3(unsigned(blocks)), dim3(kThreads), 0, stream, g);
   return 0;
 }
 int rows_any(int type, const RowsArgs& g, bool k_contiguous, hipStream_t stream) {
+  if (rows_aligned(type, g, k_contiguous)) return launch_rows_tiles(type, g, k_contiguous, stream);
   if (type == kF32) return rows_type<float>(g, k_contiguous, stream);
   if (type == kBF16) return rows_type<bf16>(g, k_contiguous, stream);
   if (type == kF16) return rows_type<f16>(g, k_contiguous, stream);
@@ -255,10 +165,10 @@ int rows_any(int type, const RowsArgs& g, bool k_contiguous, hipStream_t stream)
 }
 
 template <class T>
-int weight_type(WeightArgs g, int n, hipStream_t stream) {
+int weight_type(WeightArgs g, hipStream_t stream) {
   g.m_tiles = tiles(g.m);
   g.col_tiles = tiles(g.cols);
-  const int64_t blocks = n * g.m_tiles * g.col_tiles;
+  const int64_t blocks = g.n * g.m_tiles * g.col_tiles + kDies - 1;
   if (blocks >= (int64_t(1) << 31)) return -1;
   hipLaunchKernelGGL(weight_kernel<T>, dim3(unsigned(blocks)), dim3(kThreads), 0, stream, g);
   return 0;
@@ -267,13 +177,13 @@ int weight_type(WeightArgs g, int n, hipStream_t stream) {
 }  // namespace
 
 int launch_product_fwd(int type, const ProductArgs& p, hipStream_t stream) {
-  RowsArgs g{p.x, p.x_stride, p.source, p.k, p.m, p.w, p.w_expert, p.w_in == 1 ? p.w_out : p.w_in, p.offset, p.slots, p.n,
+  RowsArgs g{p.x, p.x_stride, p.source, divisor(p.k), p.m, p.w, p.w_expert, p.w_in == 1 ? p.w_out : p.w_in, p.offset, p.slots, p.n,
              p.ho, p.h, 0, p.out};
   return rows_any(type, g, p.w_in == 1, stream);
 }
 
 int launch_product_dx(int type, const ProductArgs& p, hipStream_t stream) {
-  RowsArgs g{p.t, p.t_stride, nullptr, 1, p.slots, p.w, p.w_expert, p.w_out == 1 ? p.w_in : p.w_out, p.offset, p.slots, p.n,
+  RowsArgs g{p.t, p.t_stride, nullptr, Divisor{}, p.slots, p.w, p.w_expert, p.w_out == 1 ? p.w_in : p.w_out, p.offset, p.slots, p.n,
              p.h, p.ho, 0, p.dx};
   return rows_any(type, g, p.w_out == 1, stream);
 }
@@ -282,12 +192,13 @@ int launch_product_dw(int type, const ProductArgs& p, hipStream_t stream) {
   // dW has the layout of w: its contiguous direction gives the columns
   WeightArgs g;
   if (p.w_in == 1)
-    g = {p.t, p.x, p.t_stride, p.x_stride, nullptr, p.source, p.k, p.slots, p.m, p.offset, p.slots, p.ho, p.h, 0, 0, p.dw};
+    g = {p.t, p.x, p.t_stride, p.x_stride, nullptr, p.source, divisor(p.k), p.slots, p.m, p.offset, p.slots, p.n, p.ho, p.h, 0, 0, p.dw};
   else
-    g = {p.x, p.t, p.x_stride, p.t_stride, p.source, nullptr, p.k, p.m, p.slots, p.offset, p.slots, p.h, p.ho, 0, 0, p.dw};
-  if (type == kF32) return weight_type<float>(g, p.n, stream);
-  if (type == kBF16) return weight_type<bf16>(g, p.n, stream);
-  if (type == kF16) return weight_type<f16>(g, p.n, stream);
+    g = {p.x, p.t, p.x_stride, p.t_stride, p.source, nullptr, divisor(p.k), p.m, p.slots, p.offset, p.slots, p.n, p.h, p.ho, 0, 0, p.dw};
+  if (weight_aligned(type, g)) return launch_weight_tiles(type, g, stream);
+  if (type == kF32) return weight_type<float>(g, stream);
+  if (type == kBF16) return weight_type<bf16>(g, stream);
+  if (type == kF16) return weight_type<f16>(g, stream);
   return -1;
 }
 

@@ -1,0 +1,158 @@
+// What the kernels of the experts' products share: matrix instructions, an expert's places, the cut of the ragged rows into
+// tiles, exact division by a constant.
+#pragma once
+
+#include "common.hpp"
+#include "experts.hpp"
+
+namespace topk {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef f16 f16x8 __attribute__((ext_vector_type(8)));
+template <class T>
+struct FragmentOf;
+template <>
+struct FragmentOf<bf16> {
+  using type = bf16x8;
+};
+template <>
+struct FragmentOf<f16> {
+  using type = f16x8;
+};
+template <>
+struct FragmentOf<float> {
+  using type = f32x4;
+};
+// 16 bytes of k of one row
+template <class T>
+using Fragment = typename FragmentOf<T>::type;
+
+// 16 x 16 outputs += 64 bytes of k: lane l holds the 16 bytes of k at (l / 16) * 16 of row l % 16 of either operand.
+// (float32 takes four instructions of one k per lane; which k meets which is the same on both sides.)
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+  return c;
+}
+
+// x / d for 0 <= x < 2^31: with s = ceil(log2 d) and M = floor(2^(31 + s) / d) + 1, M d = 2^(31 + s) + e with 0 < e <= 2^s, so
+// x M / 2^(31 + s) exceeds x / d by less than 1 / d.
+struct Divisor {
+  uint32_t mul;
+  int shift;
+};
+inline Divisor divisor(int64_t d) {
+  int s = 0;
+  while ((int64_t(1) << s) < d) ++s;
+  return {uint32_t((uint64_t(1) << (31 + s)) / uint64_t(d) + 1), 31 + s};
+}
+__device__ __forceinline__ int quotient(int x, const Divisor& d) { return int((uint64_t(uint32_t(x)) * d.mul) >> d.shift); }
+
+constexpr int kProductThreads = 256;
+
+// [begin, end) of expert e, inside [0, slots) whatever the array holds
+__device__ __forceinline__ void places(const int32_t* offset, int e, int64_t slots, int64_t* begin, int64_t* end) {
+  *begin = min(max(int64_t(offset[e]), int64_t(0)), slots);
+  *end = min(max(int64_t(offset[e + 1]), *begin), slots);
+}
+
+// The experts' rows are cut into tiles of `size` rows, one expert after the other, and every tile of rows meets
+// `col_tiles` tiles of columns.  Workgroup b is given a pair of them: the pairs lie in eight runs, one for each die (workgroups
+// are dealt to the dies in turn), so that what neighbours share is read by one die's cache.  False where there are fewer pairs
+// than workgroups.  All threads of the workgroup call it.
+struct Found {
+  int expert;
+  int64_t begin, end;      // rows
+  int64_t col;             // tile of columns
+};
+constexpr int kDies = 8;
+// pair number of workgroup b, -1 behind the last
+__device__ __forceinline__ int64_t die_order(int64_t b, int64_t total) {
+  const int64_t run = (total + kDies - 1) / kDies, i = (b % kDies) * run + b / kDies;
+  return b / kDies < run && i < total ? i : -1;
+}
+__device__ __forceinline__ bool find_tile(const int32_t* offset, int n, int64_t slots, int64_t block, int64_t col_tiles, int size,
+                                          Found* f) {
+  constexpr int kThreads = kProductThreads;
+  __shared__ int64_t wave_total[kThreads / kWave];
+  __shared__ Found found;
+  constexpr int kOwn = kExpertsMax / kThreads;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  int64_t b[kOwn], e[kOwn], mine = 0;
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    b[i] = e[i] = 0;
+    if (tid * kOwn + i < n) places(offset, tid * kOwn + i, slots, &b[i], &e[i]);
+    mine += (e[i] - b[i] + size - 1) / size;
+  }
+  int64_t scan = mine;
+  for (int off = 1; off < kWave; off <<= 1) {
+    const int64_t v = __shfl_up(scan, off, kWave);
+    if (lane >= off) scan += v;
+  }
+  if (lane == kWave - 1) wave_total[wave] = scan;
+  if (tid == 0) found.expert = -1;
+  __syncthreads();
+  int64_t start = scan - mine, total = 0;
+  for (int w = 0; w < kThreads / kWave; ++w) {
+    if (w < wave) start += wave_total[w];
+    total += wave_total[w];
+  }
+  // tiles of rows run fastest within an expert: they share its columns of W
+  const int64_t pair = die_order(block, total * col_tiles);
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    const int64_t tiles = (e[i] - b[i] + size - 1) / size;
+    if (pair >= start * col_tiles && pair < (start + tiles) * col_tiles) {
+      const int64_t in = pair - start * col_tiles, first = b[i] + in % tiles * size;
+      found = Found{tid * kOwn + i, first, min(first + size, e[i]), in / tiles};
+    }
+    start += tiles;
+  }
+  __syncthreads();
+  *f = found;
+  return f->expert >= 0;
+}
+
+// forward and dx: rows of A are places, B is W[e] seen as [n][k] (contiguous in k or in n)
+struct RowsArgs {
+  const void* a;
+  int64_t a_stride;
+  const int32_t* source;
+  Divisor div;
+  int64_t limit;
+  const void* w;
+  int64_t w_expert, w_stride;
+  const int32_t* offset;
+  int64_t slots;
+  int n;
+  int64_t cols, depth, col_tiles;
+  void* c;
+};
+// dW: k runs over an expert's places; one of the two operands goes through `source`
+struct WeightArgs {
+  const void *a, *b;
+  int64_t a_stride, b_stride;
+  const int32_t *a_source, *b_source;
+  Divisor div;
+  int64_t a_limit, b_limit;
+  const int32_t* offset;
+  int64_t slots;
+  int n;
+  int64_t m, cols, m_tiles, col_tiles;
+  void* c;
+};
+// Products whose rows are all made of whole, aligned 16-byte parts (expert_product_tiles.hip)
+bool rows_aligned(int type, const RowsArgs& g, bool k_contiguous);
+int launch_rows_tiles(int type, RowsArgs g, bool k_contiguous, hipStream_t stream);
+bool weight_aligned(int type, const WeightArgs& g);
+int launch_weight_tiles(int type, WeightArgs g, hipStream_t stream);
+
+}  // namespace topk

@@ -200,7 +200,8 @@ def test_places(gpu, rows, k, n, kind):
 
 PRODUCTS = [  # rows, k, n, h, ho
     (1, 1, 1, 1, 1), (1, 2, 4, 16, 8), (5, 2, 3, 33, 17), (40, 2, 4, 64, 64), (64, 2, 2, 128, 128), (70, 3, 5, 100, 260),
-    (300, 1, 2, 136, 72), (130, 2, 1, 31, 129), (9, 4, 40, 256, 128), (260, 2, 3, 72, 264)]
+    (300, 1, 2, 136, 72), (130, 2, 1, 31, 129), (9, 4, 40, 256, 128), (260, 2, 3, 72, 264),
+    (700, 2, 3, 328, 520)]
 
 
 def product_case(rows, k, n, h, ho, dtype, gather, wide, seed):
