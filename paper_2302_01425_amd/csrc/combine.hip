@@ -14,7 +14,7 @@ constexpr int kThreads = 256;
 template <class T, int N>
 __device__ __forceinline__ void load_part(const T* row, int64_t c, int64_t h, float (&v)[N]) {
   if (c + N <= h) {
-    const Packed<T, N> q = *reinterpret_cast<const Packed<T, N>*>(row + c);
+    const Packed<T, N> q = load_packed<T, N>(row + c);
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = to_f32(q.v[i]);
   } else {
@@ -28,7 +28,7 @@ __device__ __forceinline__ void store_part(T* row, int64_t c, int64_t h, const f
     Packed<T, N> q;
 #pragma unroll
     for (int i = 0; i < N; ++i) q.v[i] = from_f32<T>(v[i]);
-    *reinterpret_cast<Packed<T, N>*>(row + c) = q;
+    store_packed<T, N>(row + c, q);
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)

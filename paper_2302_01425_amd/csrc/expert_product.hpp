@@ -2,6 +2,8 @@
 // tiles, exact division by a constant.
 #pragma once
 
+#include <type_traits>
+
 #include "common.hpp"
 #include "experts.hpp"
 
@@ -55,32 +57,42 @@ inline Divisor divisor(int64_t d) {
 }
 __device__ __forceinline__ int quotient(int x, const Divisor& d) { return int((uint64_t(uint32_t(x)) * d.mul) >> d.shift); }
 
-constexpr int kProductThreads = 256;
-
 // [begin, end) of expert e, inside [0, slots) whatever the array holds
 __device__ __forceinline__ void places(const int32_t* offset, int e, int64_t slots, int64_t* begin, int64_t* end) {
   *begin = min(max(int64_t(offset[e]), int64_t(0)), slots);
   *end = min(max(int64_t(offset[e + 1]), *begin), slots);
 }
 
+constexpr int kDies = 8;
+
 // The experts' rows are cut into tiles of `size` rows, one expert after the other, and every tile of rows meets
-// `col_tiles` tiles of columns.  Workgroup b is given a pair of them: the pairs lie in eight runs, one for each die (workgroups
-// are dealt to the dies in turn), so that what neighbours share is read by one die's cache.  False where there are fewer pairs
-// than workgroups.  All threads of the workgroup call it.
+// `col_tiles` tiles of columns.  These pairs are dealt to the dies in runs of neighbouring ones (workgroups go to the dies in
+// turn): what neighbours share is read by one die's cache, and every die gets a share of every kind of expert.  Eight runs per
+// die where there are pairs enough, 32 pairs (a die's compute units) at most.
 struct Found {
   int expert;
   int64_t begin, end;      // rows
   int64_t col;             // tile of columns
 };
-constexpr int kDies = 8;
-// pair number of workgroup b, -1 behind the last
-__device__ __forceinline__ int64_t die_order(int64_t b, int64_t total) {
-  const int64_t run = (total + kDies - 1) / kDies, i = (b % kDies) * run + b / kDies;
-  return b / kDies < run && i < total ? i : -1;
+constexpr int kRunMost = 32;
+// pair number of workgroup b, `total` or more where there is none
+__device__ __forceinline__ int64_t dealt(int64_t b, int64_t total) {
+  const int64_t run = min(max(total / (8 * kDies), int64_t(1)), int64_t(kRunMost));
+  const int64_t die = b % kDies, i = b / kDies;
+  return (i / run * kDies + die) * run + i % run;
 }
+// Tile of the `tiles` ones of every expert that workgroup b of 8 * n * ceil(tiles / 8) takes, false where there is none: every
+// die has an eighth of every expert's, since experts differ in their rows.
+__device__ __forceinline__ bool die_share(int64_t b, int64_t tiles, int* expert, int64_t* tile) {
+  const int64_t share = (tiles + kDies - 1) / kDies, i = b / kDies;
+  *expert = int(i / share);
+  *tile = b % kDies * share + i % share;
+  return *tile < tiles;
+}
+// Expert, rows and columns of a workgroup's pair, false where there is none.  All threads of the workgroup call it.
+template <int kThreads>
 __device__ __forceinline__ bool find_tile(const int32_t* offset, int n, int64_t slots, int64_t block, int64_t col_tiles, int size,
                                           Found* f) {
-  constexpr int kThreads = kProductThreads;
   __shared__ int64_t wave_total[kThreads / kWave];
   __shared__ Found found;
   constexpr int kOwn = kExpertsMax / kThreads;
@@ -106,7 +118,7 @@ __device__ __forceinline__ bool find_tile(const int32_t* offset, int n, int64_t 
     total += wave_total[w];
   }
   // tiles of rows run fastest within an expert: they share its columns of W
-  const int64_t pair = die_order(block, total * col_tiles);
+  const int64_t pair = dealt(block, total * col_tiles);
 #pragma unroll
   for (int i = 0; i < kOwn; ++i) {
     const int64_t tiles = (e[i] - b[i] + size - 1) / size;
@@ -149,10 +161,13 @@ struct WeightArgs {
   int64_t m, cols, m_tiles, col_tiles;
   void* c;
 };
-// Products whose rows are all made of whole, aligned 16-byte parts (expert_product_tiles.hip)
-bool rows_aligned(int type, const RowsArgs& g, bool k_contiguous);
-int launch_rows_tiles(int type, RowsArgs g, bool k_contiguous, hipStream_t stream);
-bool weight_aligned(int type, const WeightArgs& g);
-int launch_weight_tiles(int type, WeightArgs g, hipStream_t stream);
+// workgroups for all pairs: as many tiles of rows as there can be, and room for the last runs
+inline int64_t rows_blocks(const RowsArgs& g, int size) {
+  return (g.slots / size + min(int64_t(g.n), g.slots)) * g.col_tiles + kDies * kRunMost;
+}
+
+int launch_rows_large(int type, RowsArgs g, bool k_contiguous, hipStream_t stream);
+int launch_rows_tiles(int type, const RowsArgs& g, bool k_contiguous, bool wide, hipStream_t stream);
+int launch_weight_tiles(int type, const WeightArgs& g, bool wide, bool direct, hipStream_t stream);
 
 }  // namespace topk

@@ -1,0 +1,111 @@
+// Forward and dx of the experts' products (expert_product.hip) where every row is made of whole, aligned 16-byte parts: tiles
+// of 256 x 256 outputs, operands loaded straight to LDS.
+//
+// A workgroup of eight wavefronts holds the tile's float32 sums in registers, 128 x 64 per wavefront: 12 fragments of 1 KB read
+// from LDS feed 32 matrix instructions.  A step is 128 bytes of k (whole cache lines of rows that are contiguous in k), 64 KB
+// of LDS for both operands, and lies in two halves: the fragments of a half are read while the other half is multiplied.  The
+// last tile of an expert's rows is one of 128 rows where it has no more.
+#include "expert_tiles.hpp"
+
+namespace topk {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kRows = 256, kCols = 256;    // of a tile (A, B)
+constexpr int kStep = 128;                 // bytes of k
+constexpr int kStageBytes = (kRows + kCols) * kStep;
+
+// One tile of ROWS x kCols.  The sum starts at step `first` and goes around: where the rows' stride is a large power of two, a
+// step of all rows lies in few memory channels, and tiles that start apart use different ones.
+template <class T, int ROWS, bool B_KC>
+__device__ __forceinline__ void rows_tile(const RowsArgs& g, const Found& f, char* lds) {
+  using IA = Image<T, true, ROWS, kThreads, kStep>;
+  using IB = Image<T, B_KC, kCols, kThreads, kStep>;
+  const int64_t n0 = f.col * kCols;
+  const T* w = static_cast<const T*>(g.w) + f.expert * g.w_expert;
+  Direct<IA, false> a;
+  a.init_rows(g.a, g.a_stride, g.source, g.div, g.limit, f.begin, f.end);
+  Direct<IB, false> b;
+  if constexpr (B_KC) b.init_rows(w, g.w_stride, nullptr, Divisor{}, 0, n0, g.cols);
+  else b.init_columns(w, g.w_stride, nullptr, n0, g.cols, 0);
+
+  const uint32_t lds0 = lds_address(lds);
+  const int wave = int(threadIdx.x) / kWave;
+  const int wm = (wave & 1) * (ROWS / 2), wn = (wave >> 1) * (kCols / 4);
+  constexpr int MI = ROWS / 2 / 16, NJ = kCols / 4 / 16;
+  f32x4 acc[MI][NJ];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  const int steps = int((g.depth + IA::kStepK - 1) / IA::kStepK);
+  int at = int(f.col * steps / g.col_tiles);               // the next step to be loaded
+  // steps behind the last are loaded as zeros
+  const auto issue = [&](int step, int stage) {
+    const int64_t k0 = int64_t(step < steps ? at : steps) * IA::kStepK;
+    at = at + 1 == steps ? 0 : at + 1;
+    a.issue(k0, g.depth, lds0 + stage * kStageBytes);
+    b.issue(k0, g.depth, lds0 + stage * kStageBytes + kRows * kStep);
+  };
+  Fragment<T> fa[2][MI], fb[2][NJ];
+  const auto read = [&](int stage, int half) {
+    const char* la = lds + stage * kStageBytes;
+    const char* lb = la + kRows * kStep;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) fa[half][i] = IA::read(la, wm + 16 * i, half);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) fb[half][j] = IB::read(lb, wn + 16 * j, half);
+  };
+  const auto multiply = [&](int half) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fb[half][j], fa[half][i], acc[i][j]);
+  };
+  issue(0, 0);
+  wait_stage<0>();
+  issue(1, 1);
+  read(0, 0);
+  for (int step = 0; step < steps; ++step) {
+    const int stage = step & 1;
+    read(stage, 1);
+    multiply(0);
+    // everything of this step is in registers, and the next step is there
+    wait_stage<0>();
+    issue(step + 2, stage);
+    read(stage ^ 1, 0);
+    multiply(1);
+  }
+  wait_stage<0>();           // (no load may reach LDS that is another workgroup's by then)
+  store_tile(acc, f.begin + wm, f.end, n0 + wn, g.cols, g.source, g.div, g.limit, static_cast<T*>(g.c), g.cols);
+}
+
+template <class T, bool B_KC>
+__global__ __launch_bounds__(kThreads, 2) void rows_large_kernel(RowsArgs g) {
+  __shared__ __attribute__((aligned(1024))) char lds[2 * kStageBytes];
+  Found f;
+  if (!find_tile<kThreads>(g.offset, g.n, g.slots, blockIdx.x, g.col_tiles, kRows, &f)) return;
+  if (f.end - f.begin <= kRows / 2) rows_tile<T, kRows / 2, B_KC>(g, f, lds);
+  else rows_tile<T, kRows, B_KC>(g, f, lds);
+}
+
+template <class T>
+int rows_type(const RowsArgs& g, bool k_contiguous, unsigned blocks, hipStream_t stream) {
+  if (k_contiguous) hipLaunchKernelGGL((rows_large_kernel<T, true>), dim3(blocks), dim3(kThreads), 0, stream, g);
+  else hipLaunchKernelGGL((rows_large_kernel<T, false>), dim3(blocks), dim3(kThreads), 0, stream, g);
+  return 0;
+}
+
+}  // namespace
+
+int launch_rows_large(int type, RowsArgs g, bool k_contiguous, hipStream_t stream) {
+  g.col_tiles = (g.cols + kCols - 1) / kCols;
+  const int64_t blocks = rows_blocks(g, kRows);
+  if (blocks >= (int64_t(1) << 31)) return -1;
+  if (type == kBF16) return rows_type<bf16>(g, k_contiguous, unsigned(blocks), stream);
+  if (type == kF16) return rows_type<f16>(g, k_contiguous, unsigned(blocks), stream);
+  return -1;
+}
+
+}  // namespace topk

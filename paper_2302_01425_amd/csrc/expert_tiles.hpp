@@ -1,0 +1,296 @@
+// Tiles of the experts' products: the images that operands have in LDS, the two ways that fill them, and how fragments of the
+// matrix instructions are read from them.
+#pragma once
+
+#include "expert_product.hpp"
+
+namespace topk {
+
+__device__ const uint4 zero_part = {0, 0, 0, 0};     // read in the place of what is out of range
+
+// LDS image of one step (STEP bytes of k) of an operand's R rows, cut into 16-byte parts.
+// KC, the operand is contiguous in k: an image row is a row of the operand.  Parts of a row change places, so that a quarter of
+// a 16-byte read (lanes 0..3, 12..15, 20..27; then 4..11, 16..19, 28..31; and so on) meets 16 different bank groups: part p of
+// row r lies at p ^ (r / 2 % 8) with rows of 128 bytes, at p ^ 3 (r / 8 % 2) with rows of 64 (p ^ (r / 4 % 4) leaves
+// conflicts of two).
+// Else an image row is one k of all R.  16-bit types are read transposed (a quarter of a wavefront reads 4 rows of 16 elements
+// and gets 4 k of one column per lane); blocks of 32 bytes change places by k % 4 and k / 8 % 2, which the eight rows read
+// at a time differ in (rows of 128 bytes: by k / 2 % 2 and k / 8 % 2, odd and even ones lie in different banks anyway).  float32
+// is read element by element; blocks of 64 bytes change places by k / 4.
+template <class T, bool KC, int R, int THREADS, int STEP>
+struct Image {
+  using Type = T;
+  static constexpr bool kKC = KC;
+  static constexpr int kThreads = THREADS;
+  static constexpr int N = 16 / sizeof(T);               // elements per part
+  static constexpr int kBytes = R * STEP;
+  static constexpr int kParts = kBytes / 16 / THREADS;   // per thread
+  static constexpr int kStepK = STEP / int(sizeof(T));
+  static constexpr int kAlong = KC ? STEP / 16 : R / N;  // parts of an image row
+
+  // Exchange of image row r, in blocks of 32 bytes (16-bit types): stays below the blocks of a row.
+  static __device__ __forceinline__ int exchange(int r) {
+    static_assert(KC || sizeof(T) == 4 || R == 64 || R >= 128, "rows of four blocks, or of eight at least");
+    static_assert(KC || sizeof(T) == 2 || R >= 64, "rows of four blocks of 64 bytes at least");
+    if constexpr (R == 64) return ((r >> 1) & 1) | ((r >> 3) & 1) << 1;
+    else return (r & 3) | ((r >> 3) & 1) << 2;
+  }
+  // the thread's part i lies at 16 (i THREADS + thread); its image row, and which part of the operand's row it is
+  static __device__ __forceinline__ int row_of(int i) { return (i * THREADS + int(threadIdx.x)) / kAlong; }
+  static __device__ __forceinline__ int part_of(int i) {
+    const int c = (i * THREADS + int(threadIdx.x)) % kAlong, r = row_of(i);
+    if constexpr (KC && STEP == 128) return c ^ ((r >> 1) & 7);
+    else if constexpr (KC) return c ^ ((r >> 3) & 1) * 3;
+    else if constexpr (sizeof(T) == 2) return c ^ exchange(r) << 1;
+    else return c ^ (((r >> 2) & 3) << 2);
+  }
+
+  // 16 bytes of k, out of the 64 from 64 * half on, of row lane % 16 of the 16 rows from r0 (a multiple of 16)
+  static __device__ __forceinline__ Fragment<T> read(const char* lds, int r0, int half) {
+    const int lane = int(threadIdx.x) & (kWave - 1), g = lane >> 4, l = lane & 15;
+    if constexpr (KC) {
+      const int part = STEP == 128 ? (half * 4 + g) ^ (l >> 1) : g ^ (l >> 3) * 3;
+      return *reinterpret_cast<const Fragment<T>*>(lds + (r0 + l) * STEP + (part << 4));
+    } else if constexpr (sizeof(T) == 2) {
+      typedef short s4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s4* Lds4;
+      const int row = half * 32 + 8 * g + (l >> 2);        // (row + 4 has the same exchange)
+      const char* at = lds + row * (R * 2) + (((r0 >> 4) ^ exchange(row)) << 5) + (l & 3) * 8;
+      union {
+        s4 half[2];
+        Fragment<T> whole;
+      } u;
+      u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)at);
+      u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(at + 4 * R * 2));
+      return u.whole;
+    } else {
+      const char* at = lds + (half * 16 + 4 * g) * (R * 4) + (((r0 >> 4) ^ g) << 6) + l * 4;
+      Fragment<T> v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const float*>(at + j * R * 4);
+      return v;
+    }
+  }
+};
+
+constexpr int kTable = 1024;               // places whose rows are looked up at a time (dW)
+
+// Rows of x behind an expert's places, kTable places at a time (dW): -1 where there is none.
+struct Table {
+  int32_t* rows;             // LDS, kTable of them
+  const int32_t* source;     // of the expert's first place
+  Divisor div;
+  int64_t limit;
+  // places k0 (a multiple of the table's size) .. of the expert's `depth`
+  template <int THREADS>
+  __device__ __forceinline__ void fill(int64_t k0, int64_t depth) const {
+    __syncthreads();
+    for (int i = threadIdx.x; i < kTable; i += THREADS) {
+      const int pair = k0 + i < depth ? source[k0 + i] : -1;
+      const int row = quotient(max(pair, 0), div);
+      rows[i] = pair >= 0 && row < limit ? row : -1;
+    }
+    __syncthreads();
+  }
+};
+
+// 16 bytes per lane from `from` to LDS at `to` (the same for the wavefront) + 16 * lane.  Not waited for, and unknown to the
+// compiler's own waits: wait_stage() counts these loads.
+__device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+// all loads to LDS but the last LEFT of this wavefront have arrived, all its accesses of LDS are done, and so for every
+// wavefront
+template <int LEFT>
+__device__ __forceinline__ void wait_stage() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const char* p) {
+  return uint32_t(uintptr_t((const __attribute__((address_space(3))) char*)p));
+}
+
+// An operand whose rows are made of whole, aligned parts, loaded to LDS without passing through registers.
+// LISTED (not KC): the row of a k is looked up in `table`.  k counts from the sum's first.
+template <class IMAGE, bool LISTED>
+struct Direct {
+  using T = typename IMAGE::Type;
+  static constexpr bool KC = IMAGE::kKC;
+  const char* p[IMAGE::kParts];    // the part at k = 0 (LISTED: its column of row 0)
+  int64_t stride;                  // bytes between rows (not KC)
+  const int32_t* table;
+
+  // Rows [first, end) of an operand contiguous in k, found through source where there is one.  Rows behind the last, and rows
+  // whose place has none, are read from another row; their outputs are not stored, or stored as zeros.
+  __device__ __forceinline__ void init_rows(const void* base, int64_t row_stride, const int32_t* source, const Divisor& d,
+                                            int64_t limit, int64_t first, int64_t end) {
+#pragma unroll
+    for (int i = 0; i < IMAGE::kParts; ++i) {
+      int64_t row = min(first + IMAGE::row_of(i), end - 1);
+      if (source != nullptr) row = min(int64_t(quotient(max(source[row], 0), d)), limit - 1);
+      p[i] = static_cast<const char*>(base) + row * row_stride * int64_t(sizeof(T)) + IMAGE::part_of(i) * 16;
+    }
+  }
+  // Columns [first, end) of an operand with one row per k, from row k_begin on; columns behind the last as above.
+  __device__ __forceinline__ void init_columns(const void* base, int64_t row_stride, const int32_t* rows, int64_t first,
+                                               int64_t end, int64_t k_begin) {
+    stride = row_stride * int64_t(sizeof(T));
+    table = rows;
+#pragma unroll
+    for (int i = 0; i < IMAGE::kParts; ++i) {
+      const int64_t at = min(first + IMAGE::part_of(i) * IMAGE::N, end - IMAGE::N);
+      p[i] = static_cast<const char*>(base) + at * int64_t(sizeof(T));
+      if (!LISTED) p[i] += (k_begin + IMAGE::row_of(i)) * stride;
+    }
+  }
+
+  // the step k0 .. to LDS at `to`, zeros from `depth` on
+  __device__ __forceinline__ void issue(int64_t k0, int64_t depth, uint32_t to) const {
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
+    const char* zeros = reinterpret_cast<const char*>(&zero_part);
+    const char* from[IMAGE::kParts];
+    if constexpr (LISTED) {
+#pragma unroll
+      for (int i = 0; i < IMAGE::kParts; ++i) {
+        const int row = table[(int(k0) + IMAGE::row_of(i)) & (kTable - 1)];
+        from[i] = row >= 0 ? p[i] + uint64_t(uint32_t(row)) * uint32_t(stride) : zeros;
+      }
+    } else {
+      const int64_t on = k0 * (KC ? int64_t(sizeof(T)) : stride);
+#pragma unroll
+      for (int i = 0; i < IMAGE::kParts; ++i) from[i] = p[i] + on;
+      if (k0 + IMAGE::kStepK > depth) {
+#pragma unroll
+        for (int i = 0; i < IMAGE::kParts; ++i)
+          if (k0 + (KC ? IMAGE::part_of(i) * IMAGE::N : IMAGE::row_of(i)) >= depth) from[i] = zeros;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < IMAGE::kParts; ++i) load_to_lds(from[i], to + (i * IMAGE::kThreads + wave * kWave) * 16);
+  }
+};
+
+// An operand of any alignment and width, loaded to registers and written to LDS a step later.
+template <class IMAGE, bool LISTED>
+struct Staged {
+  using T = typename IMAGE::Type;
+  static constexpr bool KC = IMAGE::kKC;
+  static constexpr int N = IMAGE::N;
+  const T* p[IMAGE::kParts];       // as in Direct; null: a row (a column) of zeros
+  int64_t stride;                  // elements
+  const int32_t* table;
+  int64_t edge;                    // not KC: columns from the operand's start to its end, seen from column 0 of the tile
+  Fragment<T> v[IMAGE::kParts];
+
+  __device__ __forceinline__ void init_rows(const void* base, int64_t row_stride, const int32_t* source, const Divisor& d,
+                                            int64_t limit, int64_t first, int64_t end) {
+#pragma unroll
+    for (int i = 0; i < IMAGE::kParts; ++i) {
+      int64_t row = min(first + IMAGE::row_of(i), end - 1);
+      bool there = true;
+      if (source != nullptr) {
+        const int pair = source[row];
+        row = quotient(max(pair, 0), d);
+        there = pair >= 0 && row < limit;
+      }
+      p[i] = there ? static_cast<const T*>(base) + row * row_stride + IMAGE::part_of(i) * N : nullptr;
+    }
+  }
+  __device__ __forceinline__ void init_columns(const void* base, int64_t row_stride, const int32_t* rows, int64_t first,
+                                               int64_t end, int64_t k_begin) {
+    stride = row_stride;
+    table = rows;
+    edge = end - first;
+#pragma unroll
+    for (int i = 0; i < IMAGE::kParts; ++i) {
+      p[i] = static_cast<const T*>(base) + first + IMAGE::part_of(i) * N;
+      if (!LISTED) p[i] += (k_begin + IMAGE::row_of(i)) * stride;
+    }
+  }
+
+  // the first `count` elements at `from`, zeros behind them
+  static __device__ __forceinline__ Fragment<T> some(const T* from, int64_t count) {
+    Fragment<T> q;
+#pragma unroll
+    for (int j = 0; j < N; ++j) q[j] = j < count ? from[j] : T(0.0f);
+    return q;
+  }
+  static __device__ __forceinline__ Fragment<T> whole(const T* from) {
+    const Packed<T, N> q = load_packed<T, N>(from);
+    Fragment<T> r;
+#pragma unroll
+    for (int j = 0; j < N; ++j) r[j] = q.v[j];
+    return r;
+  }
+
+  // the step k0 .. to registers, zeros from `depth` on
+  __device__ __forceinline__ void load(int64_t k0, int64_t depth) {
+    constexpr int kWide = KC ? 0 : IMAGE::kAlong * N;      // columns of the tile
+    const T* zeros = reinterpret_cast<const T*>(&zero_part);
+    const T* from[IMAGE::kParts];
+#pragma unroll
+    for (int i = 0; i < IMAGE::kParts; ++i) {
+      if constexpr (KC) {
+        from[i] = p[i] != nullptr ? p[i] + k0 : nullptr;
+      } else if constexpr (LISTED) {
+        const int row = table[(int(k0) + IMAGE::row_of(i)) & (kTable - 1)];
+        from[i] = row >= 0 ? p[i] + row * stride : nullptr;
+      } else {
+        from[i] = p[i] + k0 * stride;
+      }
+    }
+    if (k0 + IMAGE::kStepK <= depth && (KC || edge >= kWide)) {
+#pragma unroll
+      for (int i = 0; i < IMAGE::kParts; ++i) v[i] = whole(from[i] != nullptr ? from[i] : zeros);
+    } else {
+#pragma unroll
+      for (int i = 0; i < IMAGE::kParts; ++i) {
+        int64_t count = from[i] != nullptr ? N : 0;
+        if constexpr (KC) {
+          count = min(count, depth - (k0 + IMAGE::part_of(i) * N));
+        } else {
+          count = min(count, edge - IMAGE::part_of(i) * N);
+          if (k0 + IMAGE::row_of(i) >= depth) count = 0;
+        }
+        if (count >= N) v[i] = whole(from[i]);
+        else v[i] = some(from[i], count);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(char* to) const {
+#pragma unroll
+    for (int i = 0; i < IMAGE::kParts; ++i)
+      *reinterpret_cast<Fragment<T>*>(to + (i * IMAGE::kThreads + int(threadIdx.x)) * 16) = v[i];
+  }
+};
+
+// Sums of a wavefront to C: MI x NJ blocks of 16 x 16 from (m0, n0) on, below (m_end, n_end).  Lane l has row l % 16 of a block
+// and four neighbouring columns (n runs along the rows of the instruction's output).  Rows whose place has no source are zeros.
+template <class T, int MI, int NJ>
+__device__ __forceinline__ void store_tile(const f32x4 (&acc)[MI][NJ], int64_t m0, int64_t m_end, int64_t n0, int64_t n_end,
+                                           const int32_t* source, const Divisor& div, int64_t limit, T* c, int64_t c_stride) {
+  const int lane = int(threadIdx.x) & (kWave - 1);
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int64_t m = m0 + 16 * i + (lane & 15);
+    if (m >= m_end) continue;
+    bool there = true;
+    if (source != nullptr) there = source[m] >= 0 && quotient(source[m], div) < limit;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int64_t n = n0 + 16 * j + (lane >> 4) * 4;
+      T* to = c + m * c_stride + n;
+      if (n + 4 <= n_end) {
+        Packed<T, 4> q;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) q.v[r] = from_f32<T>(there ? acc[i][j][r] : 0.0f);
+        store_packed<T, 4>(to, q);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (n + r < n_end) to[r] = from_f32<T>(there ? acc[i][j][r] : 0.0f);
+      }
+    }
+  }
+}
+
+}  // namespace topk

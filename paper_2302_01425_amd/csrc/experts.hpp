@@ -100,11 +100,37 @@ __device__ __forceinline__ T from_f32(float v) {
   return T(v);
 }
 
-// N consecutive elements at an address that is a multiple of their own size only: one access, the hardware takes vector
-// accesses at any byte address
+// N consecutive elements (a power of two, up to 16 bytes) at an address that is a multiple of their own size only, as one
+// access: the hardware takes vector accesses at any byte address.  (As N elements the compiler splits them up again.)
+template <int BYTES>
+struct BitsOf;
+template <>
+struct BitsOf<4> {
+  using type = uint32_t;
+};
+template <>
+struct BitsOf<8> {
+  typedef uint32_t type __attribute__((ext_vector_type(2)));
+};
+template <>
+struct BitsOf<16> {
+  typedef uint32_t type __attribute__((ext_vector_type(4)));
+};
 template <class T, int N>
-struct __attribute__((packed, aligned(2))) Packed {
+struct Packed {
   T v[N];
 };
+template <class T, int N>
+struct __attribute__((packed, aligned(2))) Loose {
+  typename BitsOf<N * int(sizeof(T))>::type bits;
+};
+template <class T, int N>
+__device__ __forceinline__ Packed<T, N> load_packed(const T* p) {
+  return __builtin_bit_cast(Packed<T, N>, reinterpret_cast<const Loose<T, N>*>(p)->bits);
+}
+template <class T, int N>
+__device__ __forceinline__ void store_packed(T* p, const Packed<T, N>& v) {
+  reinterpret_cast<Loose<T, N>*>(p)->bits = __builtin_bit_cast(typename BitsOf<N * int(sizeof(T))>::type, v);
+}
 
 }  // namespace topk
