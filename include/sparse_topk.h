@@ -373,7 +373,7 @@ int topk_route_vjp(const void* logits, int type, int64_t stride, const int32_t* 
  *   slot_out [rows][k]: place of the pair, -1 where idx is out of [0, n) or the expert is full.
  *   source_out [rows * k]: the pair t * k + j behind a place, -1 from offset[n] on.
  *   rows * k < 2^31.  scratch: topk_expert_map_bytes(rows, k, n) bytes of the caller's for this call (TOPK_ERR_WORKSPACE if
- *   smaller), 4-byte aligned; calls that may overlap need one each.
+ *   smaller), 16-byte aligned; calls that may overlap need one each.
  */
 size_t topk_expert_map_bytes(int64_t rows, int64_t k, int64_t n);
 int topk_expert_map(const int32_t* idx, int64_t rows, int64_t k, int64_t n, int64_t capacity, int32_t* slot_out,

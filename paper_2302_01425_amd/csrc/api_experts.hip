@@ -80,7 +80,7 @@ int topk_route_vjp(const void* logits, int type, int64_t stride, const int32_t* 
 size_t topk_expert_map_bytes(int64_t rows, int64_t k, int64_t n) {
   if (rows < 0 || k < 1 || n < 1 || n > TOPK_EXPERTS_MAX || rows > (kMost - 1) / k) return 0;
   const int64_t chunks = topk::map_chunks(rows * k, int(n));
-  return chunks > 1 ? size_t(chunks) * size_t(n) * 4 : 0;
+  return chunks > 1 ? size_t(chunks) * size_t(topk::map_width(int(n))) * 4 : 0;
 }
 
 int topk_expert_map(const int32_t* idx, int64_t rows, int64_t k, int64_t n, int64_t capacity, int32_t* slot_out,
@@ -91,7 +91,7 @@ int topk_expert_map(const int32_t* idx, int64_t rows, int64_t k, int64_t n, int6
   if (rows > 0 && (idx == nullptr || slot_out == nullptr || source_out == nullptr)) return TOPK_ERR_NULL;
   const size_t need = topk_expert_map_bytes(rows, k, n);
   if (need > 0 && (scratch == nullptr || scratch_bytes < need)) return TOPK_ERR_WORKSPACE;
-  if (reinterpret_cast<uintptr_t>(scratch) % 4 != 0) return TOPK_ERR_INVALID;
+  if (reinterpret_cast<uintptr_t>(scratch) % 16 != 0) return TOPK_ERR_INVALID;
   begin();
   const topk::MapArgs a{idx, rows * k, int(n), capacity > 0 ? capacity : kMost, slot_out, source_out, offset_out, load_out,
                         static_cast<int32_t*>(scratch)};

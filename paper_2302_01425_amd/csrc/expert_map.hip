@@ -12,10 +12,11 @@
 namespace topk {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kWave;
 constexpr int64_t kChunk = 2048;       // pairs per workgroup, at least
-constexpr int kOwn = kExpertsMax / kThreads;   // experts per thread
+constexpr int kTurns = int(kChunk) / kThreads;      // pairs of a lane that stay in registers
+constexpr int kOwn = kExpertsMax / kThreads;        // experts per thread
 
 __device__ __forceinline__ int expert_of(const MapArgs& a, int64_t p, int64_t end) {
   if (p >= end) return -1;
@@ -23,9 +24,9 @@ __device__ __forceinline__ int expert_of(const MapArgs& a, int64_t p, int64_t en
   return e >= 0 && e < a.n ? e : -1;
 }
 
-__global__ __launch_bounds__(kThreads) void map_count_kernel(MapArgs a, int64_t chunk) {
-  __shared__ int32_t count[kExpertsMax];
-  for (int e = threadIdx.x; e < a.n; e += kThreads) count[e] = 0;
+__global__ __launch_bounds__(kThreads) void map_count_kernel(MapArgs a, int64_t chunk, int width) {
+  __shared__ int32_t count[kExpertsMax + 4];
+  for (int e = threadIdx.x; e < width; e += kThreads) count[e] = 0;
   __syncthreads();
   const int64_t begin = blockIdx.x * chunk, end = min(begin + chunk, a.pairs);
   for (int64_t p = begin + threadIdx.x; p < end; p += kThreads) {
@@ -33,44 +34,71 @@ __global__ __launch_bounds__(kThreads) void map_count_kernel(MapArgs a, int64_t 
     if (e >= 0) atomicAdd(&count[e], 1);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < a.n; e += kThreads) a.scratch[int64_t(blockIdx.x) * a.n + e] = count[e];
+  for (int e = threadIdx.x; e < width; e += kThreads) a.scratch[int64_t(blockIdx.x) * width + e] = count[e];
 }
 
-__global__ __launch_bounds__(kThreads) void map_place_kernel(MapArgs a, int64_t chunk, int bits) {
+// width: counts of a chunk in the scratch, n up to a multiple of four
+__global__ __launch_bounds__(kThreads) void map_place_kernel(MapArgs a, int64_t chunk, int width, int bits) {
   __shared__ int32_t next[kWaves][kExpertsMax];      // next place of an expert's pairs in a wavefront's part
-  __shared__ int32_t offset[kExpertsMax + 1];
+  __shared__ int32_t load[kExpertsMax + 4], before[kExpertsMax + 4];
   __shared__ int32_t limit[kExpertsMax];             // end of an expert's places
   __shared__ int32_t wave_total[kWaves];
+  __shared__ int32_t all;
   const int tid = threadIdx.x, wave = tid / kWave, lane = tid & (kWave - 1);
   const int64_t begin = blockIdx.x * chunk, end = min(begin + chunk, a.pairs);
   const int64_t part = (chunk + kWaves - 1) / kWaves;
   const int64_t wbegin = min(begin + wave * part, end), wend = min(wbegin + part, end);
 
-  for (int i = tid; i < kWaves * a.n; i += kThreads) next[i / a.n][i % a.n] = 0;
+  int kept_e[kTurns];                                // experts of the first turns
+#pragma unroll
+  for (int q = 0; q < kTurns; ++q) kept_e[q] = expert_of(a, wbegin + q * kWave + lane, wend);
+  for (int e = tid; e < width; e += kThreads) {
+    load[e] = before[e] = 0;
+    if (e < a.n)
+      for (int w = 0; w < kWaves; ++w) next[w][e] = 0;
+  }
   __syncthreads();
-  for (int64_t p = wbegin + lane; p < wend; p += kWave) {
+#pragma unroll
+  for (int q = 0; q < kTurns; ++q)
+    if (kept_e[q] >= 0) atomicAdd(&next[wave][kept_e[q]], 1);
+  for (int64_t p = wbegin + kTurns * kWave + lane; p < wend; p += kWave) {
     const int e = expert_of(a, p, wend);
     if (e >= 0) atomicAdd(&next[wave][e], 1);
   }
+  // counts of the chunks before this one, and of all: whole rows of counts by 16-byte reads, four experts per thread
+  if (gridDim.x > 1) {
+    const int quads = width / 4, q = tid % quads, b0 = tid / quads, step = kThreads / quads;
+    if (b0 < step) {
+      int32_t sum[4] = {0, 0, 0, 0}, mine[4] = {0, 0, 0, 0};
+#pragma unroll 8
+      for (int b = b0; b < int(gridDim.x); b += step) {
+        const int4 c = *reinterpret_cast<const int4*>(a.scratch + int64_t(b) * width + 4 * q);
+        const bool earlier = b < int(blockIdx.x);
+        sum[0] += c.x, sum[1] += c.y, sum[2] += c.z, sum[3] += c.w;
+        mine[0] += earlier ? c.x : 0, mine[1] += earlier ? c.y : 0, mine[2] += earlier ? c.z : 0, mine[3] += earlier ? c.w : 0;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        atomicAdd(&load[4 * q + i], sum[i]);
+        atomicAdd(&before[4 * q + i], mine[i]);
+      }
+    }
+  }
   __syncthreads();
 
-  // counts of the chunks before this one and of all; every thread has kOwn consecutive experts
-  int32_t before[kOwn], load[kOwn], kept[kOwn], mine = 0;
+  // every thread has kOwn consecutive experts
+  int32_t kept[kOwn], mine = 0;
 #pragma unroll
   for (int i = 0; i < kOwn; ++i) {
     const int e = tid * kOwn + i;
-    before[i] = load[i] = kept[i] = 0;
+    kept[i] = 0;
     if (e < a.n) {
       if (gridDim.x == 1) {
-        for (int w = 0; w < kWaves; ++w) load[i] += next[w][e];
-      } else {
-        for (unsigned b = 0; b < gridDim.x; ++b) {
-          const int32_t c = a.scratch[int64_t(b) * a.n + e];
-          load[i] += c;
-          if (b < blockIdx.x) before[i] += c;
-        }
+        int32_t c = 0;
+        for (int w = 0; w < kWaves; ++w) c += next[w][e];
+        load[e] = c;
       }
-      kept[i] = int32_t(min(int64_t(load[i]), a.capacity));
+      kept[i] = int32_t(min(int64_t(load[e]), a.capacity));
     }
     mine += kept[i];
   }
@@ -87,26 +115,27 @@ __global__ __launch_bounds__(kThreads) void map_place_kernel(MapArgs a, int64_t 
   for (int i = 0; i < kOwn; ++i) {
     const int e = tid * kOwn + i;
     if (e < a.n) {
-      offset[e] = start;
       limit[e] = start + kept[i];
-      int32_t at = start + before[i];                // (beyond the limit where the expert is full)
+      int32_t at = start + before[e];                // (beyond the limit where the expert is full)
       for (int w = 0; w < kWaves; ++w) {
         const int32_t c = next[w][e];
         next[w][e] = at;
         at += c;
       }
-      if (e == a.n - 1) offset[a.n] = start + kept[i];
+      if (blockIdx.x == 0) {
+        a.offset[e] = start;
+        a.load[e] = load[e];
+      }
+      if (e == a.n - 1) {
+        all = start + kept[i];
+        if (blockIdx.x == 0) a.offset[a.n] = all;
+      }
     }
     start += kept[i];
-    if (blockIdx.x == 0 && e < a.n) a.load[e] = load[i];
   }
   __syncthreads();
-  if (blockIdx.x == 0)
-    for (int e = tid; e <= a.n; e += kThreads) a.offset[e] = offset[e];
 
-  for (int64_t p0 = wbegin; p0 < wend; p0 += kWave) {
-    const int64_t p = p0 + lane;
-    const int e = expert_of(a, p, wend);
+  const auto place_pairs = [&](int64_t p, int e) {
     unsigned long long same = __ballot(e >= 0);
     for (int b = 0; b < bits; ++b) {
       const unsigned long long set = __ballot((e >> b) & 1);
@@ -123,9 +152,13 @@ __global__ __launch_bounds__(kThreads) void map_place_kernel(MapArgs a, int64_t 
     }
     if (p < wend) a.slot[p] = place;
     if (place >= 0) a.source[place] = int32_t(p);
-  }
+  };
+#pragma unroll
+  for (int q = 0; q < kTurns; ++q)
+    if (wbegin + q * kWave < wend) place_pairs(wbegin + q * kWave + lane, kept_e[q]);
+  for (int64_t p0 = wbegin + kTurns * kWave; p0 < wend; p0 += kWave) place_pairs(p0 + lane, expert_of(a, p0 + lane, wend));
   // places that nothing takes
-  for (int64_t p = max(begin, int64_t(offset[a.n])) + tid; p < end; p += kThreads) a.source[p] = -1;
+  for (int64_t p = max(begin, int64_t(all)) + tid; p < end; p += kThreads) a.source[p] = -1;
 }
 
 }  // namespace
@@ -139,10 +172,11 @@ int64_t map_chunks(int64_t pairs, int n) {
 int launch_expert_map(const MapArgs& a, hipStream_t stream) {
   const int64_t chunks = map_chunks(a.pairs, a.n);
   const int64_t chunk = max(int64_t(1), (a.pairs + chunks - 1) / chunks);
+  const int width = map_width(a.n);
   int bits = 0;
   while ((1 << bits) < a.n) ++bits;
-  if (chunks > 1) hipLaunchKernelGGL(map_count_kernel, dim3(unsigned(chunks)), dim3(kThreads), 0, stream, a, chunk);
-  hipLaunchKernelGGL(map_place_kernel, dim3(unsigned(chunks)), dim3(kThreads), 0, stream, a, chunk, bits);
+  if (chunks > 1) hipLaunchKernelGGL(map_count_kernel, dim3(unsigned(chunks)), dim3(kThreads), 0, stream, a, chunk, width);
+  hipLaunchKernelGGL(map_place_kernel, dim3(unsigned(chunks)), dim3(kThreads), 0, stream, a, chunk, width, bits);
   return 0;
 }
 

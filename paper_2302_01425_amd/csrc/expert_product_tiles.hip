@@ -36,8 +36,22 @@ using Wide = Tile<T, 128, 256, 64>;
 template <class T>
 using Small = Tile<T, 64, 64, 128>;
 
+template <class TILE>
+__device__ __forceinline__ void clear(typename TILE::Sums& acc) {
+#pragma unroll
+  for (int i = 0; i < TILE::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < TILE::NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+}
+
+// float32 sums of a step are added to the others' as a whole: a sum over k then has roundings of k / 32 additions, and those
+// of 32, instead of k in a row (16-bit outputs are rounded by more than either)
 template <class TILE, class IA, class IB>
-__device__ __forceinline__ void multiply(const char* stage, typename TILE::Sums& acc) {
+__device__ __forceinline__ void multiply(const char* stage, typename TILE::Sums& sums) {
+  constexpr bool kApart = sizeof(typename TILE::T) == 4;
+  typename TILE::Sums step;
+  typename TILE::Sums& acc = kApart ? step : sums;
+  if constexpr (kApart) clear<TILE>(step);
 #pragma unroll
   for (int half = 0; half < TILE::kStep / 64; ++half) {
     Fragment<typename TILE::T> fa[TILE::MI], fb[TILE::NJ];
@@ -49,6 +63,12 @@ __device__ __forceinline__ void multiply(const char* stage, typename TILE::Sums&
     for (int j = 0; j < TILE::NJ; ++j)
 #pragma unroll
       for (int i = 0; i < TILE::MI; ++i) acc[i][j] = mma(fb[j], fa[i], acc[i][j]);
+  }
+  if constexpr (kApart) {
+#pragma unroll
+    for (int i = 0; i < TILE::MI; ++i)
+#pragma unroll
+      for (int j = 0; j < TILE::NJ; ++j) sums[i][j] += step[i][j];
   }
 }
 
@@ -98,14 +118,6 @@ __device__ __forceinline__ void sum_staged(char* lds, LA& a, LB& b, const Table&
     multiply<TILE, IA, IB>(lds + stage * TILE::kStageBytes, acc);
     stage ^= 1;
   }
-}
-
-template <class TILE>
-__device__ __forceinline__ void clear(typename TILE::Sums& acc) {
-#pragma unroll
-  for (int i = 0; i < TILE::MI; ++i)
-#pragma unroll
-    for (int j = 0; j < TILE::NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 }
 
 template <class TILE, bool B_KC>

@@ -51,6 +51,7 @@ struct MapArgs {
   int32_t* scratch;
 };
 int64_t map_chunks(int64_t pairs, int n);
+inline int map_width(int n) { return (n + 3) / 4 * 4; }      // counts of a chunk in the scratch (16-byte rows)
 int launch_expert_map(const MapArgs& a, hipStream_t stream);
 
 // One product over the ragged groups.  Operand strides are in elements; w(e, o, i) = w[e * w_expert + o * w_out + i * w_in].

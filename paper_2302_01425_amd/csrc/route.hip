@@ -3,7 +3,7 @@
 //   the `keep` best of `groups` equal groups stay (score of a group: the sum of its `top` largest c),
 //   idx = the k largest c in descending order, equal ones by ascending index, val = scale s[idx] (/ sum of the chosen s).
 // A logit of -inf or NaN, or a bias of -inf or NaN, takes its expert out; where fewer than k are left, idx = -1, val = 0.
-// Scores that are compared are float64: the choice jumps where two scores cross, and two float32 scores of 16384 x 256
+// Scores are compared as float64 would: the choice jumps where two scores cross, and two float32 scores of 16384 x 256
 // cross within their rounding a few times per call.  Logits are compared as they are.
 #include <cmath>
 
@@ -16,15 +16,17 @@ namespace {
 constexpr int kThreads = 256;
 constexpr float kNone = -INFINITY;
 
+__device__ __forceinline__ float max_of(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }   // (no NaN)
+__device__ __forceinline__ double max_of(double a, double b) { return max_f64(a, b); }
 template <int GL, int LM = GL / 2>
 __device__ __forceinline__ float group_max(float v) {
   if constexpr (LM == 0) return v;
-  else return group_max<GL, LM / 2>(fmaxf(v, __uint_as_float(lane_xor<LM>(__float_as_uint(v)))));
+  else return group_max<GL, LM / 2>(max_of(v, __uint_as_float(lane_xor<LM>(__float_as_uint(v)))));
 }
 template <int GL, int LM = GL / 2>
 __device__ __forceinline__ double group_max(double v) {
   if constexpr (LM == 0) return v;
-  else return group_max<GL, LM / 2>(fmax(v, lane_xor_f64<LM>(v)));
+  else return group_max<GL, LM / 2>(max_of(v, lane_xor_f64<LM>(v)));
 }
 template <int GL, int LM = GL / 2>
 __device__ __forceinline__ float group_sum_f32(float v) {
@@ -42,152 +44,251 @@ __device__ __forceinline__ float sigmoid_over(float l, float m) {
   return expf(fminf(l, 0.0f) - m) / (1.0f + expf(-fabsf(l)));
 }
 
-// GL lanes per row, E elements per lane.  Lanes are dealt to the groups first (`lanes` consecutive ones each, a power of
-// two), so that a group's scores are reduced by a butterfly over its own lanes; a lane holds consecutive elements, so that
-// the lowest lane and the lowest register hold the lowest index.
-template <class T, int GL, int E, class KEY>
-__global__ __launch_bounds__(kThreads) void route_fwd_kernel(RouteArgs a, int lanes) {
-  const int64_t row = (int64_t(blockIdx.x) * kThreads + threadIdx.x) / GL;
-  if (row >= a.rows) return;                                       // (whole row groups)
-  const int lr = int(threadIdx.x) & (GL - 1);
-  const int size = a.n / a.groups, g = lr / lanes, in = (lr & (lanes - 1)) * E;
-  const int count = g < a.groups ? min(max(size - in, 0), E) : 0;  // elements of this lane
-  const int base = g * size + in;
-  const T* lp = static_cast<const T*>(a.logits) + row * a.stride + base;
-  float l[E];
+// E consecutive elements as float, `fill` behind the first `count`
+template <class T, int E>
+__device__ __forceinline__ void load_row_part(const T* p, int count, float fill, float (&v)[E]) {
+  if (count == E) {
+    constexpr int N = E * sizeof(T) < 16 ? E : 16 / int(sizeof(T));
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    l[e] = e < count ? to_f32(lp[e]) : kNone;
-    if (isnan(l[e])) l[e] = kNone;
-  }
-  float top = l[0];
+    for (int c = 0; c < E; c += N) {
+      const Packed<T, N> q = load_packed<T, N>(p + c);
 #pragma unroll
-  for (int e = 1; e < E; ++e) top = fmaxf(top, l[e]);
-  top = group_max<GL>(top);
-
-  // what is compared
-  KEY key[E];
-  if constexpr (sizeof(KEY) == 8) {
-    double total = 1.0;
-    if (a.score == kSoftmax) {
-      double z = 0.0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        key[e] = l[e] == kNone ? 0.0 : exp_below(double(l[e]), double(top));
-        z += key[e];
-      }
-      total = group_sum_f64<GL>(z);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) key[e] = 1.0 / (1.0 + exp(-double(l[e])));
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float b = a.bias != nullptr && e < count ? a.bias[base + e] : 0.0f;
-      const bool out = l[e] == kNone || !(b > kNone);
-      key[e] = out ? -INFINITY : key[e] / total + double(b);
+      for (int i = 0; i < N; ++i) v[c + i] = to_f32(q.v[i]);
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) key[e] = l[e];
+    for (int e = 0; e < E; ++e) v[e] = e < count ? to_f32(p[e]) : fill;
   }
+}
+template <class T, int E>
+__device__ __forceinline__ void store_row_part(T* p, int count, const float (&v)[E]) {
+  if (count == E) {
+    constexpr int N = E * sizeof(T) < 16 ? E : 16 / int(sizeof(T));
+#pragma unroll
+    for (int c = 0; c < E; c += N) {
+      Packed<T, N> q;
+#pragma unroll
+      for (int i = 0; i < N; ++i) q.v[i] = from_f32<T>(v[c + i]);
+      store_packed<T, N>(p + c, q);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (e < count) p[e] = from_f32<T>(v[e]);
+  }
+}
 
+// What a lane knows of its row.  Lanes are dealt to the groups first (`lanes` consecutive ones each, a power of two), so that
+// a group's scores are reduced by a butterfly over its own lanes; a lane holds consecutive elements, so that the lowest lane
+// and the lowest register hold the lowest index.
+template <int E>
+struct Lane {
+  float l[E];        // logits, -inf where there is none
+  float b[E];        // bias
+  float top;         // the row's largest logit
+  int g, lanes, lr;
+};
+
+__device__ __forceinline__ float max3_of(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+template <int E>
+__device__ __forceinline__ float max_all(const float (&v)[E]) {
+  float m = v[E - 1];                    // (E is even)
+#pragma unroll
+  for (int e = 0; e + 1 < E; e += 2) m = max3_of(m, v[e], v[e + 1]);
+  return m;
+}
+template <int E>
+__device__ __forceinline__ double max_all(const double (&v)[E]) {
+  double m = v[0];
+#pragma unroll
+  for (int e = 1; e < E; ++e) m = max_of(m, v[e]);
+  return m;
+}
+
+// A chosen element: score, logit, bias, index.
+struct Record {
+  float c, l, b;
+  int i;
+};
+
+// The k largest and the next one to line[] (LDS, k + 1 records of the row), in order; returns how many there are.  KEY float:
+// `sure` says whether float64 would choose the same.  `base`: index of the lane's first element.
+template <int GL, int E, class KEY>
+__device__ __forceinline__ int choose(const RouteArgs& a, const Lane<E>& w, bool scored, int base, Record* line, bool* sure) {
+  KEY key[E];
+  float err = 0.0f;                      // bound of a float32 score's error
+  if (scored) {
+    if (a.score == kSoftmax) {
+      KEY z = KEY(0);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        key[e] = w.l[e] == kNone ? KEY(0) : exp_below(KEY(w.l[e]), KEY(w.top));
+        z += key[e];
+      }
+      if constexpr (sizeof(KEY) == 8) z = group_sum_f64<GL>(z);
+      else z = group_sum_f32<GL>(z);
+      z = KEY(1) / z;
+#pragma unroll
+      for (int e = 0; e < E; ++e) key[e] *= z;
+      // s <= 1: the sum's 38 roundings and 7 of its terms', 5 of exponential, quotient and product, and (top - l) s <= 1 / e of
+      // the difference's
+      err = 56 * 0x1p-24f;
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if constexpr (sizeof(KEY) == 8) key[e] = 1.0 / (1.0 + exp(-double(w.l[e])));
+        else key[e] = 1.0f / (1.0f + expf(-w.l[e]));
+      }
+      // s (1 - s) of the exponential's 2, s of the sum's and the quotient's
+      err = 4 * 0x1p-24f;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const bool out = w.l[e] == kNone || !(w.b[e] > kNone);
+      key[e] = out ? KEY(-INFINITY) : key[e] + KEY(w.b[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) key[e] = KEY(w.l[e]);
+  }
+  bool good = true;
   if (a.groups > 1) {
     KEY first = -INFINITY, second = -INFINITY;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const KEY v = key[e];
-      second = fmax(second, fmin(first, v));
-      first = fmax(first, v);
+      second = max_of(second, fmin(first, key[e]));
+      first = max_of(first, key[e]);
     }
-    for (int off = 1; off < lanes; off <<= 1) {
+    for (int off = 1; off < w.lanes; off <<= 1) {
       const KEY f = __shfl_xor(first, off, GL), s = __shfl_xor(second, off, GL);
-      second = fmax(fmax(second, s), fmin(first, f));
-      first = fmax(first, f);
+      second = max_of(max_of(second, s), fmin(first, f));
+      first = max_of(first, f);
     }
     const KEY score = a.top == 2 && second > KEY(-INFINITY) ? first + second : first;
     int rank = 0;
     for (int o = 0; o < a.groups; ++o) {
-      const KEY other = __shfl(score, o * lanes, GL);
-      rank += other > score || (other == score && o < g);
+      const KEY other = __shfl(score, o * w.lanes, GL);
+      rank += other > score || (other == score && o < w.g);
+    }
+    if (sizeof(KEY) == 4 && scored) {
+      const float in = rank < a.keep ? float(score) : INFINITY, out = rank < a.keep || w.g >= a.groups ? kNone : float(score);
+      const float low = -group_max<GL>(-in), high = group_max<GL>(out);
+      good = high == kNone || low - high > 2.0f * (2.0f * err + 0x1p-23f * (1.0f + fabsf(low) + fabsf(high)));
     }
     if (rank >= a.keep) {
 #pragma unroll
       for (int e = 0; e < E; ++e) key[e] = -INFINITY;
     }
-    if constexpr (sizeof(KEY) == 8) {
-      if (a.bias == nullptr) {           // sums of scores chose the groups, the logits choose in them
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (key[e] > -INFINITY) key[e] = double(l[e]);
-      }
-    }
-  }
-
-  // k times the largest of the row that is left
-  int place[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) place[e] = -1;
-  int found = 0;
-  const int lane0 = int(threadIdx.x) & (kWave - 1) & ~(GL - 1);
-  for (int j = 0; j < a.k; ++j) {
-    KEY best = key[0];
-    int at = 0;
-#pragma unroll
-    for (int e = 1; e < E; ++e)
-      if (key[e] > best) {
-        best = key[e];
-        at = e;
-      }
-    const KEY m = group_max<GL>(best);
-    if (!(m > KEY(-INFINITY))) continue;
-    found = j + 1;
-    const unsigned long long who = __ballot(best == m) >> lane0;
-    if (lr == __ffsll(GL < 64 ? who & ((1ull << (GL & 63)) - 1ull) : who) - 1) {
+    if (scored && a.bias == nullptr) {     // sums of scores chose the groups, the logits choose in them
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (e == at) {
-          place[e] = j;
-          key[e] = -INFINITY;
-        }
+        if (key[e] > KEY(-INFINITY)) key[e] = KEY(w.l[e]);
     }
   }
 
-  // their weights
-  float u[E], sum = 0.0f, factor;
-  if (a.renorm) {
-    float m = kNone;
+  const bool check = sizeof(KEY) == 4 && scored && a.bias != nullptr;
+  KEY score[E];
+  int place[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (place[e] >= 0) m = fmaxf(m, a.score == kSoftmax ? l[e] : fminf(l[e], 0.0f));
-    m = group_max<GL>(m);
+  for (int e = 0; e < E; ++e) {
+    score[e] = key[e];
+    place[e] = -1;
+  }
+  int found = 0;
+  const int lane0 = int(threadIdx.x) & (kWave - 1) & ~(GL - 1);
+  const int rounds = check ? min(a.k + 1, a.n) : a.k;
+  for (int j = 0; j < rounds; ++j) {
+    const KEY best = max_all(key);
+    const KEY m = group_max<GL>(best);
+    const bool any = m > KEY(-INFINITY);
+    const unsigned long long who = __ballot(best == m) >> lane0;
+    bool mine = any && w.lr == __ffsll(GL < 64 ? who & ((1ull << (GL & 63)) - 1ull) : who) - 1;
+    found += any;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      u[e] = place[e] < 0 ? 0.0f : a.score == kSoftmax ? exp_below(l[e], m) : sigmoid_over(l[e], m);
-      sum += u[e];
+      const bool hit = mine & (key[e] == m);
+      place[e] = hit ? j : place[e];
+      key[e] = hit ? KEY(-INFINITY) : key[e];
+      mine = mine & !hit;
     }
-    factor = a.scale / group_sum_f32<GL>(sum);
-  } else if (a.score == kSoftmax) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      u[e] = l[e] == kNone ? 0.0f : exp_below(l[e], top);
-      sum += u[e];
-    }
-    factor = a.scale / group_sum_f32<GL>(sum);
-  } else {
-#pragma unroll
-    for (int e = 0; e < E; ++e) u[e] = sigmoid_over(l[e], 0.0f);
-    factor = a.scale;
   }
 #pragma unroll
   for (int e = 0; e < E; ++e)
-    if (place[e] >= 0) {
-      a.idx[row * a.k + place[e]] = base + e;
-      a.val[row * a.k + place[e]] = u[e] * factor;
+    if (place[e] >= 0) line[place[e]] = Record{float(score[e]), w.l[e], w.b[e], base + e};
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");           // (other lanes read the records)
+  if (check) {
+    // neighbours in the order closer than their errors, unless they are ties
+    for (int j = w.lr; j + 1 < found; j += GL) {
+      const Record p = line[j], q = line[j + 1];
+      const bool tie = p.l == q.l && p.b == q.b;
+      if (!tie && !(p.c - q.c > 2.0f * (err + 0x1p-23f * (1.0f + fabsf(p.c))))) good = false;
     }
-  for (int j = found + lr; j < a.k; j += GL) {
-    a.idx[row * a.k + j] = -1;
-    a.val[row * a.k + j] = 0.0f;
+  }
+  if (sizeof(KEY) == 4 && scored) {
+    const unsigned long long bad = __ballot(!good) >> lane0;
+    good = (GL < 64 ? bad & ((1ull << (GL & 63)) - 1ull) : bad) == 0ull;
+  }
+  *sure = good;
+  return min(found, a.k);
+}
+
+// GL lanes per row, E elements per lane
+template <class T, int GL, int E>
+__global__ __launch_bounds__(kThreads) void route_fwd_kernel(RouteArgs a, int lanes) {
+  __shared__ __attribute__((aligned(16))) Record lines[kThreads / GL][kChoicesMax + 1];
+  const int64_t row = (int64_t(blockIdx.x) * kThreads + threadIdx.x) / GL;
+  if (row >= a.rows) return;                                       // (whole row groups; no barrier below)
+  Lane<E> w;
+  w.lr = int(threadIdx.x) & (GL - 1);
+  w.lanes = lanes;
+  w.g = w.lr / lanes;
+  const int size = a.n / a.groups, in = (w.lr & (lanes - 1)) * E;
+  const int count = w.g < a.groups ? min(max(size - in, 0), E) : 0;  // elements of this lane
+  const int base = w.g * size + in;
+  load_row_part<T, E>(static_cast<const T*>(a.logits) + row * a.stride + base, count, kNone, w.l);
+  if (a.bias != nullptr) load_row_part<float, E>(a.bias + base, count, 0.0f, w.b);
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (a.bias == nullptr) w.b[e] = 0.0f;
+    if (isnan(w.l[e])) w.l[e] = kNone;
+  }
+  w.top = group_max<GL>(max_all(w.l));
+
+  // Scores, not logits, are compared where a bias is added or scores of a group are.  Float32 decides where its errors leave no
+  // doubt, float64 elsewhere (8192 x 256 with sigmoid scores, k = 8: about one row in a thousand).
+  const bool scored = a.bias != nullptr || (a.groups > 1 && a.top == 2);
+  bool sure;
+  Record* line = lines[threadIdx.x / GL];
+  int found = choose<GL, E, float>(a, w, scored, base, line, &sure);
+  if (scored && !sure) found = choose<GL, E, double>(a, w, scored, base, line, &sure);
+
+  // their weights: lane q takes the choices q, q + GL, ..
+  float m = 0.0f, sum = 0.0f;
+  if (a.renorm) {
+    m = kNone;
+    for (int j = w.lr; j < found; j += GL) m = max_of(m, a.score == kSoftmax ? line[j].l : fminf(line[j].l, 0.0f));
+    m = group_max<GL>(m);
+    for (int j = w.lr; j < found; j += GL) sum += a.score == kSoftmax ? exp_below(line[j].l, m) : sigmoid_over(line[j].l, m);
+    sum = group_sum_f32<GL>(sum);
+  } else if (a.score == kSoftmax) {
+    m = w.top;
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum += w.l[e] == kNone ? 0.0f : exp_below(w.l[e], m);
+    sum = group_sum_f32<GL>(sum);
+  } else {
+    sum = 1.0f;
+  }
+  const float factor = a.scale / sum;
+  for (int j = w.lr; j < a.k; j += GL) {
+    const bool there = j < found;
+    const float l = there ? line[j].l : 0.0f;
+    const float u = a.score == kSoftmax ? exp_below(l, m) : sigmoid_over(l, m);
+    a.idx[row * a.k + j] = there ? line[j].i : -1;
+    a.val[row * a.k + j] = there ? u * factor : 0.0f;
   }
 }
 
@@ -197,111 +298,117 @@ __global__ __launch_bounds__(kThreads) void route_fwd_kernel(RouteArgs a, int la
 //   softmax                 dl[idx_j] += scale w_j t_j,  dl -= scale s mean
 //   sigmoid, renormalised   dl[idx_j] += scale w_j (1 - s_j) (t_j - mean)
 //   sigmoid                 dl[idx_j] += scale s_j (1 - s_j) t_j
+// Lane q of a row takes the choices q, q + GL, ..: their terms are then handed to the lanes that hold the entries.  Only
+// softmax that is not renormalised reads the whole row.
 template <class T, int GL, int E>
 __global__ __launch_bounds__(kThreads) void route_vjp_kernel(RouteVjpArgs a) {
+  constexpr int J = kChoicesMax / GL;                              // choices of a lane, at most
   const int64_t row = (int64_t(blockIdx.x) * kThreads + threadIdx.x) / GL;
   if (row >= a.rows) return;
   const int lr = int(threadIdx.x) & (GL - 1);
   const int base = lr * E, count = min(max(a.n - base, 0), E);
   const T* lp = static_cast<const T*>(a.logits) + row * a.stride;
-  const int32_t* ip = a.idx + row * a.k;
-  const float* tp = a.cotangent + row * a.k;
   const bool whole = a.score == kSoftmax && !a.renorm;
+  int at[J];
+  float l[J], t[J];
+#pragma unroll
+  for (int q = 0; q < J; ++q) {
+    at[q] = -1;
+    l[q] = kNone;
+    t[q] = 0.0f;
+    const int j = q * GL + lr;
+    if (q * GL < a.k && j < a.k) {
+      at[q] = a.idx[row * a.k + j];
+      if (at[q] < 0 || at[q] >= a.n) at[q] = -1;
+      if (at[q] >= 0) {
+        l[q] = to_f32(lp[at[q]]);
+        t[q] = a.cotangent[row * a.k + j];
+      }
+      if (!(l[q] > kNone)) {                                       // -inf, NaN: an expert that is out has weight 0
+        l[q] = kNone;
+        t[q] = 0.0f;
+      }
+    }
+  }
   float s[E];
-  float m = kNone, sum = 0.0f;
+  float m = kNone;
+  double sum = 0.0, mean = 0.0;
   if (whole) {
+    load_row_part<T, E>(lp + base, count, kNone, s);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      s[e] = e < count ? to_f32(lp[base + e]) : kNone;
       if (isnan(s[e])) s[e] = kNone;
-      m = fmaxf(m, s[e]);
+      m = max_of(m, s[e]);
     }
     m = group_max<GL>(m);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      s[e] = s[e] == kNone ? 0.0f : exp_below(s[e], m);
-      sum += s[e];
-    }
-    sum = group_sum_f32<GL>(sum);
-  } else {
+    for (int e = 0; e < E; ++e) s[e] = s[e] == kNone ? 0.0f : exp_below(s[e], m);
 #pragma unroll
-    for (int e = 0; e < E; ++e) s[e] = 0.0f;
-    if (a.renorm) {
-      for (int j = 0; j < a.k; ++j) {
-        const int i = ip[j];
-        if (i < 0 || i >= a.n) continue;
-        const float l = to_f32(lp[i]);
-        if (!isnan(l)) m = fmaxf(m, a.score == kSoftmax ? l : fminf(l, 0.0f));
-      }
-    } else {
-      m = 0.0f;
-    }
-  }
-  // unnormalised weight of choice j (0: an empty place, or an expert that is out)
-  const auto weight = [&](float l) -> float {
-    if (!(l > kNone)) return 0.0f;
-    return a.score == kSoftmax ? exp_below(l, m) : sigmoid_over(l, m);
-  };
-  float mean = 0.0f;
-  if (whole || a.renorm) {
-    float chosen = 0.0f;
-    for (int j = 0; j < a.k; ++j) {
-      const int i = ip[j];
-      if (i < 0 || i >= a.n) continue;
-      const float w = weight(to_f32(lp[i]));
-      chosen += w;
-      if (w > 0.0f) mean += w * tp[j];
-    }
-    if (!whole) sum = chosen;
+    for (int e = 0; e < E; e += 4) sum += double((s[e] + s[e + 1]) + (s[e + 2] + s[e + 3]));
+  } else if (a.renorm) {
+#pragma unroll
+    for (int q = 0; q < J; ++q) m = max_of(m, a.score == kSoftmax ? l[q] : fminf(l[q], 0.0f));
+    m = group_max<GL>(m);
   } else {
-    sum = 1.0f;
+    m = 0.0f;
   }
-  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  float w[J];
+#pragma unroll
+  for (int q = 0; q < J; ++q) {
+    w[q] = l[q] == kNone ? 0.0f : a.score == kSoftmax ? exp_below(l[q], m) : sigmoid_over(l[q], m);
+    mean += double(w[q]) * double(t[q]);
+    if (!whole) sum += double(w[q]);
+  }
+  if (whole || a.renorm) {
+    sum = group_sum_f64<GL>(sum);
+    mean = group_sum_f64<GL>(mean);
+  } else {
+    sum = 1.0;
+  }
+  const double inv = sum > 0.0 ? 1.0 / sum : 0.0;
   mean *= inv;
+  const float less = float(-inv * mean);
   float d[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) d[e] = whole ? -s[e] * inv * mean : 0.0f;
-  for (int j = 0; j < a.k; ++j) {
-    const int i = ip[j];
-    if (i < 0 || i >= a.n) continue;
-    const float l = to_f32(lp[i]);
-    const float w = weight(l) * inv;
-    if (!(w > 0.0f)) continue;
-    float v = w * (a.renorm ? tp[j] - mean : tp[j]);
-    if (a.score == kSigmoid) v *= sigmoid_over(-l, 0.0f);
+  for (int e = 0; e < E; ++e) d[e] = whole ? s[e] * less : 0.0f;
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (base + e == i) d[e] += v;
+  for (int q = 0; q < J; ++q) {
+    if (q * GL >= a.k) break;
+    float v = float(double(w[q]) * inv * (a.renorm ? double(t[q]) - mean : double(t[q])));
+    if (a.score == kSigmoid && l[q] > kNone) v *= sigmoid_over(-l[q], 0.0f);
+    const int here = min(a.k - q * GL, GL);
+    for (int j = 0; j < here; ++j) {
+      const int i = __shfl(at[q], j, GL) - base;
+      const float add = __shfl(v, j, GL);
+#pragma unroll
+      for (int e = 0; e < E; ++e) d[e] += i == e ? add : 0.0f;
+    }
   }
-  T* gp = static_cast<T*>(a.grad) + row * a.n + base;
 #pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (e < count) gp[e] = from_f32<T>(a.scale * d[e]);
+  for (int e = 0; e < E; ++e) d[e] *= a.scale;
+  store_row_part<T, E>(static_cast<T*>(a.grad) + row * a.n + base, count, d);
 }
 
 template <class T, int GL, int E>
-void fwd(const RouteArgs& a, int lanes, bool f64, hipStream_t stream) {
+void fwd(const RouteArgs& a, int padded, hipStream_t stream) {
   const dim3 grid(unsigned((a.rows * GL + kThreads - 1) / kThreads));
-  if (f64) hipLaunchKernelGGL((route_fwd_kernel<T, GL, E, double>), grid, dim3(kThreads), 0, stream, a, lanes);
-  else hipLaunchKernelGGL((route_fwd_kernel<T, GL, E, float>), grid, dim3(kThreads), 0, stream, a, lanes);
+  hipLaunchKernelGGL((route_fwd_kernel<T, GL, E>), grid, dim3(kThreads), 0, stream, a, GL / padded);
 }
 
 template <class T>
 int fwd_type(const RouteArgs& a, hipStream_t stream) {
-  // scores, not logits, are compared where a bias is added or scores of a group are
-  const bool f64 = a.bias != nullptr || (a.groups > 1 && a.top == 2);
   int padded = 1;                        // groups, up to a power of two
   while (padded < a.groups) padded *= 2;
   const int size = a.n / a.groups;
   // the fewest lanes whose registers hold a row: the k rounds cost a reduction over the lanes each
   const auto fits = [&](int gl, int e) { return padded <= gl && size <= gl / padded * e; };
-  if (fits(8, 4)) fwd<T, 8, 4>(a, 8 / padded, f64, stream);
-  else if (fits(8, 8)) fwd<T, 8, 8>(a, 8 / padded, f64, stream);
-  else if (fits(16, 8)) fwd<T, 16, 8>(a, 16 / padded, f64, stream);
-  else if (fits(32, 8)) fwd<T, 32, 8>(a, 32 / padded, f64, stream);
-  else if (fits(64, 8)) fwd<T, 64, 8>(a, 64 / padded, f64, stream);
-  else if (fits(64, 16)) fwd<T, 64, 16>(a, 64 / padded, f64, stream);
-  else if (fits(64, 32)) fwd<T, 64, 32>(a, 64 / padded, f64, stream);
+  if (fits(8, 4)) fwd<T, 8, 4>(a, padded, stream);
+  else if (fits(8, 8)) fwd<T, 8, 8>(a, padded, stream);
+  else if (fits(16, 8)) fwd<T, 16, 8>(a, padded, stream);
+  else if (fits(32, 8)) fwd<T, 32, 8>(a, padded, stream);
+  else if (fits(64, 8)) fwd<T, 64, 8>(a, padded, stream);
+  else if (fits(64, 16)) fwd<T, 64, 16>(a, padded, stream);
+  else if (fits(64, 32)) fwd<T, 64, 32>(a, padded, stream);
   else return -1;
   return 0;
 }
