@@ -107,9 +107,12 @@ def load() -> ctypes.CDLL:
 _call = None
 _CALL_ENTRIES = ("topk_mask_fwd", "topk_mask_jvp", "topk_mask_vjp", "topkmag_fwd", "topkmag_jvp", "topkmag_vjp",
                  "topk_signed_mask_fwd", "topk_signed_mask_jvp", "topk_masked_value_fwd", "topk_masked_value_jvp",
-                 "topk_mask_sparse_fwd", "topk_mask_loss")
+                 "topk_mask_sparse_fwd", "topk_mask_loss", "topk_route_fwd", "topk_route_vjp", "topk_expert_map",
+                 "topk_expert_map_bytes", "topk_expert_product_fwd", "topk_expert_product_vjp", "topk_combine_fwd",
+                 "topk_combine_vjp")
 (_MASK_FWD, _MASK_JVP, _MASK_VJP, _MAG_FWD, _MAG_JVP, _MAG_VJP, _SIGNED_FWD, _SIGNED_JVP, _MASKED_FWD, _MASKED_JVP,
- _SPARSE, _LOSS) = range(len(_CALL_ENTRIES))
+ _SPARSE, _LOSS, _ROUTE_FWD, _ROUTE_VJP, _MAP, _MAP_BYTES, _PRODUCT_FWD, _PRODUCT_VJP, _COMBINE_FWD,
+ _COMBINE_VJP) = range(len(_CALL_ENTRIES))
 
 
 def _load_call(L: ctypes.CDLL) -> None:
@@ -640,6 +643,10 @@ def _new(t, shape, dtype, ref):
 def topk_route_fwd(logits, k, score=TOPK_SCORE_SOFTMAX, bias=None, groups=1, keep_groups=1, group_top=1,
                    renormalise=True, scale=1.0, idx_out=None, val_out=None, stream=None):
     """Returns (idx [rows, k] int32, val [rows, k] float32)."""
+    if _call is not None and idx_out is None and val_out is None:
+        r = _call.route_fwd(_ROUTE_FWD, logits, k, score, bias, groups, keep_groups, group_top, renormalise, scale, stream)
+        if r is not None:
+            return r
     logits = _rows(logits, "logits")
     rows, n = logits.shape
     k = int(k)
@@ -667,6 +674,10 @@ def topk_route_fwd(logits, k, score=TOPK_SCORE_SOFTMAX, bias=None, groups=1, kee
 def topk_route_vjp(logits, idx, cotangent, score=TOPK_SCORE_SOFTMAX, renormalise=True, scale=1.0, grad_out=None,
                    stream=None):
     """Returns the gradient in the logits, [rows, n] of their type, of the weights at the chosen idx [rows, k]."""
+    if _call is not None and grad_out is None:
+        r = _call.route_vjp(_ROUTE_VJP, logits, idx, cotangent, score, renormalise, scale, stream)
+        if r is not None:
+            return r
     logits = _rows(logits, "logits")
     rows, n = logits.shape
     if not isinstance(idx, torch.Tensor) or idx.dim() != 2:
@@ -689,6 +700,10 @@ def topk_route_vjp(logits, idx, cotangent, score=TOPK_SCORE_SOFTMAX, renormalise
 
 def topk_expert_map(idx, n, capacity=0, slot_out=None, source_out=None, offset_out=None, load_out=None, stream=None):
     """Returns (slot [rows, k], source [rows * k], offset [n + 1], load [n]), int32, for the chosen experts idx [rows, k]."""
+    if _call is not None and slot_out is None and source_out is None and offset_out is None and load_out is None:
+        r = _call.expert_map(_MAP, _MAP_BYTES, idx, n, capacity, stream)
+        if r is not None:
+            return r
     if not isinstance(idx, torch.Tensor) or not idx.is_cuda or idx.dim() != 2:
         raise TopkError("idx must be a 2-D int32 tensor [rows, k] in GPU memory")
     rows, k = idx.shape
@@ -744,6 +759,10 @@ def _product(x, w, offset, source, k):
 def topk_expert_product_fwd(x, w, offset, source=None, k=1, out=None, stream=None):
     """Returns out [slots, ho]: W[e] x[source // k] for every place, w [n, ho, h]; without source the rows of x are in expert
     order.  Rows behind offset[n] are not written."""
+    if _call is not None and out is None:
+        r = _call.product_fwd(_PRODUCT_FWD, x, w, offset, source, k, stream)
+        if r is not None:
+            return r
     x, slots, n, h, ho, _, args = _product(x, w, offset, source, k)
     if out is not None:
         _exact(out, (slots, ho), x.dtype, x, "out")
@@ -760,6 +779,10 @@ def topk_expert_product_vjp(x, w, offset, cotangent, source=None, k=1, want_x=Tr
                             stream=None):
     """Returns (dx [slots, h] per place, dw like w); one that is not wanted is None.  Rows of dx behind offset[n] are not
     written; with source, topk_combine_fwd(dx, slot) gives the gradient of x."""
+    if _call is not None and dx_out is None and dw_out is None:
+        r = _call.product_vjp(_PRODUCT_VJP, x, w, offset, source, k, cotangent, want_x, want_w, stream)
+        if r is not None:
+            return r
     x, slots, n, h, ho, plain, args = _product(x, w, offset, source, k)
     cotangent = _rows(cotangent, "cotangent", x)
     if tuple(cotangent.shape) != (slots, ho):
@@ -797,6 +820,10 @@ def _combine(y, slot, val):
 
 def topk_combine_fwd(y, slot, val=None, out=None, stream=None):
     """Returns out [rows, h]: the sum over j of val[t, j] * y[slot[t, j]] (val None: ones)."""
+    if _call is not None and out is None:
+        r = _call.combine_fwd(_COMBINE_FWD, y, slot, val, stream)
+        if r is not None:
+            return r
     y, rows, k, slots, h = _combine(y, slot, val)
     if out is not None:
         _exact(out, (rows, h), y.dtype, y, "out")
@@ -813,6 +840,10 @@ def topk_combine_fwd(y, slot, val=None, out=None, stream=None):
 
 def topk_combine_vjp(y, slot, val, cotangent, dy_out=None, dval_out=None, stream=None):
     """Returns (dy [slots, h], dval [rows, k]; None with val None).  Rows of dy that no pair names are not written."""
+    if _call is not None and dval_out is None:
+        r = _call.combine_vjp(_COMBINE_VJP, y, slot, val, cotangent, dy_out, stream)
+        if r is not None:
+            return r
     y, rows, k, slots, h = _combine(y, slot, val)
     cotangent = _rows(cotangent, "cotangent", y)
     if tuple(cotangent.shape) != (rows, h):

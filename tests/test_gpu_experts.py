@@ -534,3 +534,59 @@ def test_refusals(gpu):
             call()
             raise AssertionError(f"call {j} was not refused")
     torch.cuda.synchronize()
+
+
+def test_native_step_and_python_agree(gpu):
+    """Results, errors and returned objects of the binding's native step against the Python code behind it."""
+    import torch
+    from tests.test_gpu_native_call import both as compare
+    assert gpu._call is not None, "the native call path was not built"
+
+    def both(f):
+        def tensors():
+            r = f()
+            r = r if isinstance(r, tuple) else (r,)
+            return tuple(t for t in r if t is not None) + (sum(t is None for t in r),)
+        return compare(gpu, tensors)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        l = torch.randn((70, 24), generator=g, device="cuda").to(dtype)
+        wide = torch.randn((70, 30), generator=g, device="cuda").to(dtype)[:, 3:27]
+        bias, t = torch.randn(24, generator=g, device="cuda"), torch.randn((70, 2), generator=g, device="cuda")
+        for x in (l, wide, l[:0], l.t().contiguous().t()):
+            both(lambda: gpu.topk_route_fwd(x, 2))
+            both(lambda: gpu.topk_route_fwd(x, 3, gpu.TOPK_SCORE_SIGMOID, bias=bias, groups=4, keep_groups=2, group_top=2,
+                                            renormalise=False, scale=2))
+        idx, val = gpu.topk_route_fwd(l, 2)
+        both(lambda: gpu.topk_route_vjp(wide, idx, t, renormalise=False))
+        both(lambda: gpu.topk_route_vjp(l, idx, t, 1, scale=0.5))
+        both(lambda: gpu.topk_expert_map(idx, 24))
+        both(lambda: gpu.topk_expert_map(idx.expand(70, 2)[:0], 24, capacity=1))
+        both(lambda: gpu.topk_expert_map(idx.repeat(100, 1), 24, capacity=7))
+        slot, source, offset, load = gpu.topk_expert_map(idx, 24)
+        x, w = torch.randn((70, 16), generator=g, device="cuda").to(dtype), torch.randn((24, 8, 16), generator=g, device="cuda").to(dtype)
+        c = torch.randn((140, 8), generator=g, device="cuda").to(dtype)
+        for u in (w, w.transpose(1, 2).contiguous().transpose(1, 2), w[:, :, :1], w[:, :1]):
+            xu = x[:, :u.shape[2]]
+            both(lambda: gpu.topk_expert_product_fwd(xu, u, offset, source, 2))
+            cu = c[:, :u.shape[1]]
+            for want in ((True, True), (True, False), (False, True), (False, False)):
+                both(lambda: gpu.topk_expert_product_vjp(xu, u, offset, cu, source, 2, *want))
+        y = gpu.topk_expert_product_fwd(x, w, offset, source, 2)
+        out = torch.randn((70, 8), generator=g, device="cuda").to(dtype)
+        dy = torch.zeros_like(y)
+        both(lambda: gpu.topk_combine_fwd(y, slot, val))
+        both(lambda: gpu.topk_combine_fwd(y, slot))
+        both(lambda: gpu.topk_combine_vjp(y, slot, val, out))
+        both(lambda: gpu.topk_combine_vjp(y, slot, None, out, dy_out=dy))
+        assert gpu.topk_combine_vjp(y, slot, val, out, dy_out=dy)[0] is dy
+        for bad in (lambda: gpu.topk_route_fwd(l, 25), lambda: gpu.topk_route_fwd(l, -1), lambda: gpu.topk_route_fwd(l, 2, 7),
+                    lambda: gpu.topk_route_fwd(l, 2, groups=5), lambda: gpu.topk_route_fwd(l.cpu(), 2),
+                    lambda: gpu.topk_route_fwd(l, 2, bias=bias[:5]), lambda: gpu.topk_route_vjp(l, idx[:5], t),
+                    lambda: gpu.topk_expert_map(idx, 0), lambda: gpu.topk_expert_map(idx.long(), 24),
+                    lambda: gpu.topk_expert_product_fwd(x, w, offset[:3], source, 2),
+                    lambda: gpu.topk_expert_product_fwd(x, w, offset, source, 0),
+                    lambda: gpu.topk_expert_product_vjp(x, w, offset, c[:5], source, 2), lambda: gpu.topk_combine_fwd(y, slot, val[:4]),
+                    lambda: gpu.topk_combine_vjp(y, slot, val, out, dy_out=y), lambda: gpu.topk_combine_vjp(y, slot, val, out[:5])):
+            r = compare(gpu, bad)
+            assert isinstance(r[0], type) and issubclass(r[0], gpu.TopkError), r
