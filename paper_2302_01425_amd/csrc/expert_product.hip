@@ -26,24 +26,22 @@ int64_t row_tiles(const RowsArgs& g, int64_t rows, int64_t cols) {
   return min(int64_t(g.n), g.slots) * cut(even_share(g.slots, g.n), rows) * cut(g.cols, cols);
 }
 
-// Which kernel takes the rows (bfloat16, us; 64 x 64 / 128 x 256 / 256 x 256):
+// Which kernel takes the rows (bfloat16, us):
 //   float32: 64 x 64, bound by the matrix unit already.
-//   whole parts, 2048 -> 4096, 16 experts of 8, 64, 128, 256 rows on average: 37 / 58 / 41, 60 / 76 / 68, 99 / 84 / 78,
-//     170 / 140 / 116; 8 experts of 128 rows, 1024 -> 1024, 32 tiles of 256 x 256: 16 / 34 / 34; 16 of 250, 1000 -> 2008, 128
-//     tiles: 55 / 47 / 40.
-//   others, 64 x 64 / 128 x 256: 1025 -> 2047, 64 experts of 64 rows 110 / 117, of 256 282 / 216 (and 2047 -> 1025, where 256
-//     columns leave a fifth of the last tiles empty, 291 / 322); 16 of 250 rows, 1001 -> 2005 67 / 59, 2005 -> 1001 (128 tiles)
-//     92 / 149.
+//   whole parts, 64 x 64 / 256 x 256: 2048 -> 4096, 16 experts of 8, 64, 128, 256 rows on average 37 / 41, 60 / 68, 99 / 78,
+//     170 / 116; 8 experts of 128 rows, 1024 -> 1024, 32 tiles of 256 x 256: 16 / 34; 16 of 250, 1000 -> 2008, 128 tiles 55 / 40.
+//   others, 64 x 64 / 128 x 128: 64 experts of 32 rows, 1025 -> 2047 68 / 78, of 256 278 / 225; 16 of 250, 1001 -> 2005 (512 tiles)
+//     63 / 56, 2005 -> 1001 (256 tiles) 90 / 94; 40 of 70, 777 -> 333 16 / 24.
 int launch_rows(int type, const RowsArgs& g, bool k_contiguous, hipStream_t stream) {
-  if (type == kF32) return launch_rows_tiles(type, g, k_contiguous, false, stream);
+  if (type == kF32) return launch_rows_tiles(type, g, k_contiguous, kSmall, stream);
   const int64_t share = even_share(g.slots, g.n);
   const int s = size_of(type);
   // (limit 0: there is no row that could be read in the place of one that is out of range)
   const bool whole = g.limit > 0 && whole_parts(g.a, g.a_stride, g.depth, s) &&
                      whole_parts(g.w, g.w_stride, k_contiguous ? g.depth : g.cols, s) && g.w_expert * s % 16 == 0;
   if (whole && share >= 96 && row_tiles(g, 256, 256) >= 96) return launch_rows_large(type, g, k_contiguous, stream);
-  const bool wide = share >= 128 && row_tiles(g, 128, 256) >= 256 && cut(g.cols, 256) * 256 * 8 <= g.cols * 9;
-  return launch_rows_tiles(type, g, k_contiguous, wide, stream);
+  const bool middle = share >= 128 && row_tiles(g, 128, 128) >= 400;
+  return launch_rows_tiles(type, g, k_contiguous, middle ? kMiddle : kSmall, stream);
 }
 
 }  // namespace
@@ -72,12 +70,12 @@ int launch_product_dw(int type, const ProductArgs& p, hipStream_t stream) {
   const int s = size_of(type);
   const bool whole = whole_parts(g.a, g.a_stride, g.m, s) && whole_parts(g.b, g.b_stride, g.cols, s) &&
                      g.a_stride * s < (int64_t(1) << 32) && g.b_stride * s < (int64_t(1) << 32);   // (32-bit products of rows)
-  // Tiles of 128 x 256 (bfloat16, us; 64 x 64 / 128 x 256).  Whole parts, 64 experts of 16, 64, 256 rows, 2048 x 1024: 122 / 89,
-  // 159 / 106, 281 / 172; 8 of 128, 1024 x 1024, 256 tiles: 19 / 20.  Others, 1025 x 2047: 169 / 156, 219 / 193, 384 / 400; 16 of
-  // 250 rows, 1001 x 2005 79 / 115; 40 of 70 rows, 777 x 333, 480 tiles 23 / 42.
-  const int64_t tiles = p.n * cut(g.m, 128) * cut(g.cols, 256);
-  const bool wide = whole ? tiles >= 256 : even_share(p.slots, p.n) <= 64 && tiles >= 1024;
-  return launch_weight_tiles(type, g, wide, whole, stream);
+  // (bfloat16, us)  Whole parts, 64 x 64 / 128 x 256: 64 experts of 16, 64, 256 rows, 2048 x 1024 122 / 89, 159 / 106, 281 / 172; 8
+  // of 128, 1024 x 1024, 256 tiles: 19 / 20.  Others, 64 x 64 / 128 x 128: 1025 x 2047, 64 experts of 32 rows 184 / 153, of 256
+  // 375 / 347; 16 of 250 rows, 1001 x 2005, 2048 tiles 77 / 84; 8 of 8, 2047 x 2047, 2048 tiles 50 / 43; 40 of 70 rows, 777 x 333, 840
+  // tiles 23 / 30.
+  if (whole && p.n * cut(g.m, 128) * cut(g.cols, 256) >= 256) return launch_weight_tiles(type, g, kWideDirect, stream);
+  return launch_weight_tiles(type, g, p.n * cut(g.m, 128) * cut(g.cols, 128) >= 2048 ? kMiddle : kSmall, stream);
 }
 
 }  // namespace topk

@@ -167,7 +167,9 @@ inline int64_t rows_blocks(const RowsArgs& g, int size) {
 }
 
 int launch_rows_large(int type, RowsArgs g, bool k_contiguous, hipStream_t stream);
-int launch_rows_tiles(int type, const RowsArgs& g, bool k_contiguous, bool wide, hipStream_t stream);
-int launch_weight_tiles(int type, const WeightArgs& g, bool wide, bool direct, hipStream_t stream);
+// tiles of expert_product_tiles.hip; kWideDirect: dW of whole, aligned parts only.  float32 takes kSmall
+enum TileKind { kSmall, kMiddle, kWideDirect };
+int launch_rows_tiles(int type, const RowsArgs& g, bool k_contiguous, TileKind kind, hipStream_t stream);
+int launch_weight_tiles(int type, const WeightArgs& g, TileKind kind, hipStream_t stream);
 
 }  // namespace topk

@@ -1,14 +1,13 @@
-// The experts' products (expert_product.hip) in tiles of 128 x 256 and of 64 x 64 outputs, by workgroups of four wavefronts:
-// dW, and forward and dx of rows of any alignment and of few tiles.
+// The experts' products (expert_product.hip) by workgroups of four wavefronts: dW, and forward and dx of rows of any alignment
+// and of few tiles.
 //
-// 128 x 256: 64 x 128 float32 sums per wavefront, 12 fragments of 1 KB read from LDS feed 32 matrix instructions.  A step is
-// 64 bytes of k, 24 KB of LDS for both operands, so that two workgroups share a compute unit and one multiplies while the
-// other begins, ends or waits: an expert's rows (the k of dW) are few.
-// 64 x 64: 32 x 32 sums per wavefront, steps of 128 bytes, 16 KB; five workgroups share a compute unit.  For float32, whose
-// matrix instructions take 16 times as long for the same fragments, and where tiles of the other size would leave compute
-// units without work.
-// Operands made of whole, aligned parts are loaded straight to LDS two steps ahead (three images) in the tiles of 128 x 256 of
-// dW; else they pass through registers, one step ahead (two images).
+// Wide, 128 x 256: 64 x 128 float32 sums per wavefront, 12 fragments of 1 KB read from LDS feed 32 matrix instructions.  A step
+// is 64 bytes of k, 24 KB of LDS for both operands, so that two workgroups share a compute unit and one multiplies while the
+// other begins, ends or waits: an expert's rows (the k of dW) are few.  For dW of whole, aligned parts, which are loaded
+// straight to LDS two steps ahead (three images).
+// Middle, 128 x 128 (steps of 64 bytes), and Small, 64 x 64 (of 128 bytes), of any alignment: operands pass through registers,
+// two steps ahead, to two images of 16 KB; three and four workgroups share a compute unit.  Small is for float32, whose matrix
+// instructions take 16 times as long for the same fragments, and where larger tiles would leave compute units without work.
 #include "expert_tiles.hpp"
 
 namespace topk {
@@ -33,6 +32,8 @@ struct Tile {
 };
 template <class T>
 using Wide = Tile<T, 128, 256, 64>;
+template <class T>
+using Middle = Tile<T, 128, 128, 64>;
 template <class T>
 using Small = Tile<T, 64, 64, 128>;
 
@@ -100,23 +101,29 @@ __device__ __forceinline__ void sum_direct(char* lds, const LA& a, const LB& b, 
 template <class TILE, class IA, class IB, bool LISTED, class LA, class LB>
 __device__ __forceinline__ void sum_staged(char* lds, LA& a, LB& b, const Table& table, int64_t depth,
                                            typename TILE::Sums& acc) {
-  const auto load = [&](int64_t k0) {
+  const auto load = [&](int set, int64_t k0) {
+    if (k0 >= depth) return;
     if constexpr (LISTED) {
       if ((k0 & (kTable - 1)) == 0) table.fill<kThreads>(k0, depth);
     }
-    a.load(k0, depth);
-    b.load(k0, depth);
+    a.load(set, k0, depth);
+    b.load(set, k0, depth);
   };
-  load(0);
-  int stage = 0;
-  for (int64_t k0 = 0; k0 < depth; k0 += IA::kStepK) {
-    // (the image that is written was read two steps ago, and a barrier lies between)
-    a.store(lds + stage * TILE::kStageBytes);
-    b.store(lds + stage * TILE::kStageBytes + IA::kBytes);
-    __syncthreads();
-    if (k0 + IA::kStepK < depth) load(k0 + IA::kStepK);
-    multiply<TILE, IA, IB>(lds + stage * TILE::kStageBytes, acc);
-    stage ^= 1;
+  load(0, 0);
+  load(1, IA::kStepK);
+  for (int64_t k0 = 0; k0 < depth; k0 += 2 * IA::kStepK) {
+#pragma unroll
+    for (int set = 0; set < 2; ++set) {
+      const int64_t k = k0 + set * IA::kStepK;
+      if (k >= depth) break;
+      // (the image that is written was read two steps ago, and a barrier lies between)
+      char* image = lds + set * TILE::kStageBytes;
+      a.store(set, image);
+      b.store(set, image + IA::kBytes);
+      __syncthreads();
+      load(set, k + 2 * IA::kStepK);
+      multiply<TILE, IA, IB>(image, acc);
+    }
   }
 }
 
@@ -196,26 +203,28 @@ int weight_tile(WeightArgs g, hipStream_t stream) {
   return 0;
 }
 template <class T>
-int weight_type(const WeightArgs& g, bool wide, bool direct, hipStream_t stream) {
-  if (!wide) return weight_tile<Small<T>, false>(g, stream);
-  return direct ? weight_tile<Wide<T>, true>(g, stream) : weight_tile<Wide<T>, false>(g, stream);
+int rows_type(const RowsArgs& g, bool k_contiguous, bool middle, hipStream_t stream) {
+  return middle ? rows_tile<Middle<T>>(g, k_contiguous, stream) : rows_tile<Small<T>>(g, k_contiguous, stream);
+}
+template <class T>
+int weight_type(const WeightArgs& g, TileKind kind, hipStream_t stream) {
+  if (kind == kWideDirect) return weight_tile<Wide<T>, true>(g, stream);
+  return kind == kMiddle ? weight_tile<Middle<T>, false>(g, stream) : weight_tile<Small<T>, false>(g, stream);
 }
 
 }  // namespace
 
-int launch_rows_tiles(int type, const RowsArgs& g, bool k_contiguous, bool wide, hipStream_t stream) {
+int launch_rows_tiles(int type, const RowsArgs& g, bool k_contiguous, TileKind kind, hipStream_t stream) {
   if (type == kF32) return rows_tile<Small<float>>(g, k_contiguous, stream);
-  if (type == kBF16)
-    return wide ? rows_tile<Wide<bf16>>(g, k_contiguous, stream) : rows_tile<Small<bf16>>(g, k_contiguous, stream);
-  if (type == kF16)
-    return wide ? rows_tile<Wide<f16>>(g, k_contiguous, stream) : rows_tile<Small<f16>>(g, k_contiguous, stream);
+  if (type == kBF16) return rows_type<bf16>(g, k_contiguous, kind == kMiddle, stream);
+  if (type == kF16) return rows_type<f16>(g, k_contiguous, kind == kMiddle, stream);
   return -1;
 }
 
-int launch_weight_tiles(int type, const WeightArgs& g, bool wide, bool direct, hipStream_t stream) {
+int launch_weight_tiles(int type, const WeightArgs& g, TileKind kind, hipStream_t stream) {
   if (type == kF32) return weight_tile<Small<float>, false>(g, stream);
-  if (type == kBF16) return weight_type<bf16>(g, wide, direct, stream);
-  if (type == kF16) return weight_type<f16>(g, wide, direct, stream);
+  if (type == kBF16) return weight_type<bf16>(g, kind, stream);
+  if (type == kF16) return weight_type<f16>(g, kind, stream);
   return -1;
 }
 

@@ -143,33 +143,28 @@ struct Direct {
     }
   }
 
-  // the step k0 .. to LDS at `to`, zeros from `depth` on
-  __device__ __forceinline__ void issue(int64_t k0, int64_t depth, uint32_t to) const {
+  // part i of the step k0 .. to LDS at `to` (of the step's image), zeros from `depth` on; without branches
+  __device__ __forceinline__ void issue_part(int i, int64_t k0, int64_t depth, uint32_t to) const {
     const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
     const char* zeros = reinterpret_cast<const char*>(&zero_part);
-    const char* from[IMAGE::kParts];
+    const char* from;
     if constexpr (LISTED) {
-#pragma unroll
-      for (int i = 0; i < IMAGE::kParts; ++i) {
-        const int row = table[(int(k0) + IMAGE::row_of(i)) & (kTable - 1)];
-        from[i] = row >= 0 ? p[i] + uint64_t(uint32_t(row)) * uint32_t(stride) : zeros;
-      }
+      const int row = table[(int(k0) + IMAGE::row_of(i)) & (kTable - 1)];
+      from = row >= 0 ? p[i] + uint64_t(uint32_t(row)) * uint32_t(stride) : zeros;
     } else {
-      const int64_t on = k0 * (KC ? int64_t(sizeof(T)) : stride);
-#pragma unroll
-      for (int i = 0; i < IMAGE::kParts; ++i) from[i] = p[i] + on;
-      if (k0 + IMAGE::kStepK > depth) {
-#pragma unroll
-        for (int i = 0; i < IMAGE::kParts; ++i)
-          if (k0 + (KC ? IMAGE::part_of(i) * IMAGE::N : IMAGE::row_of(i)) >= depth) from[i] = zeros;
-      }
+      from = p[i] + k0 * (KC ? int64_t(sizeof(T)) : stride);
+      const int left = int(min(depth - k0, int64_t(IMAGE::kStepK)));
+      from = (KC ? IMAGE::part_of(i) * IMAGE::N : IMAGE::row_of(i)) < left ? from : zeros;
     }
+    load_to_lds(from, to + (i * IMAGE::kThreads + wave * kWave) * 16);
+  }
+  __device__ __forceinline__ void issue(int64_t k0, int64_t depth, uint32_t to) const {
 #pragma unroll
-    for (int i = 0; i < IMAGE::kParts; ++i) load_to_lds(from[i], to + (i * IMAGE::kThreads + wave * kWave) * 16);
+    for (int i = 0; i < IMAGE::kParts; ++i) issue_part(i, k0, depth, to);
   }
 };
 
-// An operand of any alignment and width, loaded to registers and written to LDS a step later.
+// An operand of any alignment and width, loaded to one of two sets of registers and written to LDS two steps later.
 template <class IMAGE, bool LISTED>
 struct Staged {
   using T = typename IMAGE::Type;
@@ -179,7 +174,7 @@ struct Staged {
   int64_t stride;                  // elements
   const int32_t* table;
   int64_t edge;                    // not KC: columns from the operand's start to its end, seen from column 0 of the tile
-  Fragment<T> v[IMAGE::kParts];
+  Fragment<T> v[2][IMAGE::kParts];
 
   __device__ __forceinline__ void init_rows(const void* base, int64_t row_stride, const int32_t* source, const Divisor& d,
                                             int64_t limit, int64_t first, int64_t end) {
@@ -222,8 +217,8 @@ struct Staged {
     return r;
   }
 
-  // the step k0 .. to registers, zeros from `depth` on
-  __device__ __forceinline__ void load(int64_t k0, int64_t depth) {
+  // the step k0 .. to the registers `set`, zeros from `depth` on
+  __device__ __forceinline__ void load(int set, int64_t k0, int64_t depth) {
     constexpr int kWide = KC ? 0 : IMAGE::kAlong * N;      // columns of the tile
     const T* zeros = reinterpret_cast<const T*>(&zero_part);
     const T* from[IMAGE::kParts];
@@ -240,7 +235,7 @@ struct Staged {
     }
     if (k0 + IMAGE::kStepK <= depth && (KC || edge >= kWide)) {
 #pragma unroll
-      for (int i = 0; i < IMAGE::kParts; ++i) v[i] = whole(from[i] != nullptr ? from[i] : zeros);
+      for (int i = 0; i < IMAGE::kParts; ++i) v[set][i] = whole(from[i] != nullptr ? from[i] : zeros);
     } else {
 #pragma unroll
       for (int i = 0; i < IMAGE::kParts; ++i) {
@@ -251,15 +246,15 @@ struct Staged {
           count = min(count, edge - IMAGE::part_of(i) * N);
           if (k0 + IMAGE::row_of(i) >= depth) count = 0;
         }
-        if (count >= N) v[i] = whole(from[i]);
-        else v[i] = some(from[i], count);
+        if (count >= N) v[set][i] = whole(from[i]);
+        else v[set][i] = some(from[i], count);
       }
     }
   }
-  __device__ __forceinline__ void store(char* to) const {
+  __device__ __forceinline__ void store(int set, char* to) const {
 #pragma unroll
     for (int i = 0; i < IMAGE::kParts; ++i)
-      *reinterpret_cast<Fragment<T>*>(to + (i * IMAGE::kThreads + int(threadIdx.x)) * 16) = v[i];
+      *reinterpret_cast<Fragment<T>*>(to + (i * IMAGE::kThreads + int(threadIdx.x)) * 16) = v[set][i];
   }
 };
 
