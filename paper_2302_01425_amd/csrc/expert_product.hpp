@@ -32,16 +32,17 @@ using Fragment = typename FragmentOf<T>::type;
 
 // 16 x 16 outputs += 64 bytes of k: lane l holds the 16 bytes of k at (l / 16) * 16 of row l % 16 of either operand.
 // (float32 takes four instructions of one k per lane; which k meets which is the same on both sides.)
-__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
+// instruction `q` of kMma of them
+template <class T>
+constexpr int kMma = sizeof(T) == 4 ? 4 : 1;
+__device__ __forceinline__ f32x4 mma(int, bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) {
+__device__ __forceinline__ f32x4 mma(int, f16x8 a, f16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
-  return c;
+__device__ __forceinline__ f32x4 mma(int q, f32x4 a, f32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a[q], b[q], c, 0, 0, 0);
 }
 
 // x / d for 0 <= x < 2^31: with s = ceil(log2 d) and M = floor(2^(31 + s) / d) + 1, M d = 2^(31 + s) + e with 0 < e <= 2^s, so

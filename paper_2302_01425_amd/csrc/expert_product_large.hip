@@ -61,7 +61,7 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& g, const Found& f, cha
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fb[half][j], fa[half][i], acc[i][j]);
+      for (int j = 0; j < NJ; ++j) acc[i][j] = mma(0, fb[half][j], fa[half][i], acc[i][j]);
   };
   issue(0, 0);
   wait_stage<0>();

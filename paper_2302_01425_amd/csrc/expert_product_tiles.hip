@@ -45,14 +45,8 @@ __device__ __forceinline__ void clear(typename TILE::Sums& acc) {
     for (int j = 0; j < TILE::NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 }
 
-// float32 sums of a step are added to the others' as a whole: a sum over k then has roundings of k / 32 additions, and those
-// of 32, instead of k in a row (16-bit outputs are rounded by more than either)
 template <class TILE, class IA, class IB>
-__device__ __forceinline__ void multiply(const char* stage, typename TILE::Sums& sums) {
-  constexpr bool kApart = sizeof(typename TILE::T) == 4;
-  typename TILE::Sums step;
-  typename TILE::Sums& acc = kApart ? step : sums;
-  if constexpr (kApart) clear<TILE>(step);
+__device__ __forceinline__ void multiply(const char* stage, typename TILE::Sums& acc) {
 #pragma unroll
   for (int half = 0; half < TILE::kStep / 64; ++half) {
     Fragment<typename TILE::T> fa[TILE::MI], fb[TILE::NJ];
@@ -60,16 +54,13 @@ __device__ __forceinline__ void multiply(const char* stage, typename TILE::Sums&
     for (int i = 0; i < TILE::MI; ++i) fa[i] = IA::read(stage, TILE::wave_row() + 16 * i, half);
 #pragma unroll
     for (int j = 0; j < TILE::NJ; ++j) fb[j] = IB::read(stage + IA::kBytes, TILE::wave_col() + 16 * j, half);
+    // (the instructions that add to the same sums lie apart)
 #pragma unroll
-    for (int j = 0; j < TILE::NJ; ++j)
+    for (int q = 0; q < kMma<typename TILE::T>; ++q)
 #pragma unroll
-      for (int i = 0; i < TILE::MI; ++i) acc[i][j] = mma(fb[j], fa[i], acc[i][j]);
-  }
-  if constexpr (kApart) {
+      for (int j = 0; j < TILE::NJ; ++j)
 #pragma unroll
-    for (int i = 0; i < TILE::MI; ++i)
-#pragma unroll
-      for (int j = 0; j < TILE::NJ; ++j) sums[i][j] += step[i][j];
+        for (int i = 0; i < TILE::MI; ++i) acc[i][j] = mma(q, fb[j], fa[i], acc[i][j]);
   }
 }
 
@@ -98,9 +89,22 @@ __device__ __forceinline__ void sum_direct(char* lds, const LA& a, const LB& b, 
   wait_stage<0>();           // (no load may reach LDS that is another workgroup's by then)
 }
 
+// float32 sums of four steps, 128 k, are added to the others' as a whole: a sum over k then has roundings of k / 128 additions,
+// and those of 128, instead of k in a row.  (16-bit outputs are rounded by more than either.)
 template <class TILE, class IA, class IB, bool LISTED, class LA, class LB>
 __device__ __forceinline__ void sum_staged(char* lds, LA& a, LB& b, const Table& table, int64_t depth,
-                                           typename TILE::Sums& acc) {
+                                           typename TILE::Sums& sums) {
+  constexpr bool kApart = sizeof(typename TILE::T) == 4;
+  typename TILE::Sums part;
+  typename TILE::Sums& acc = kApart ? part : sums;
+  if constexpr (kApart) clear<TILE>(part);
+  const auto add_part = [&]() {
+#pragma unroll
+    for (int i = 0; i < TILE::MI; ++i)
+#pragma unroll
+      for (int j = 0; j < TILE::NJ; ++j) sums[i][j] += part[i][j];
+    clear<TILE>(part);
+  };
   const auto load = [&](int set, int64_t k0) {
     if (k0 >= depth) return;
     if constexpr (LISTED) {
@@ -124,7 +128,9 @@ __device__ __forceinline__ void sum_staged(char* lds, LA& a, LB& b, const Table&
       load(set, k + 2 * IA::kStepK);
       multiply<TILE, IA, IB>(image, acc);
     }
+    if (kApart && (k0 & (2 * IA::kStepK)) != 0) add_part();
   }
+  if constexpr (kApart) add_part();
 }
 
 template <class TILE, bool B_KC>

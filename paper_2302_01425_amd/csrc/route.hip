@@ -120,7 +120,7 @@ struct Record {
 template <int GL, int E, class KEY>
 __device__ __forceinline__ int choose(const RouteArgs& a, const Lane<E>& w, bool scored, int base, Record* line, bool* sure) {
   KEY key[E];
-  float err = 0.0f;                      // bound of a float32 score's error
+  float rel = 0.0f, err = 0.0f;          // a float32 score s is off by rel s + err at most
   if (scored) {
     if (a.score == kSoftmax) {
       KEY z = KEY(0);
@@ -134,17 +134,18 @@ __device__ __forceinline__ int choose(const RouteArgs& a, const Lane<E>& w, bool
       z = KEY(1) / z;
 #pragma unroll
       for (int e = 0; e < E; ++e) key[e] *= z;
-      // s <= 1: the sum's 38 roundings and 7 of its terms', 5 of exponential, quotient and product, and (top - l) s <= 1 / e of
-      // the difference's
-      err = 56 * 0x1p-24f;
+      // E + 6 roundings of the sum and ln n < 7 of its terms', 5 of exponential, quotient and product; and (top - l) s <= 1 / e
+      // of the difference's
+      rel = (E + 18) * 0x1p-24f;
+      err = 0.5f * 0x1p-24f;
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         if constexpr (sizeof(KEY) == 8) key[e] = 1.0 / (1.0 + exp(-double(w.l[e])));
         else key[e] = 1.0f / (1.0f + expf(-w.l[e]));
       }
-      // s (1 - s) of the exponential's 2, s of the sum's and the quotient's
-      err = 4 * 0x1p-24f;
+      // 2 of the exponential, 1 of the sum, 2 of the quotient
+      rel = 5 * 0x1p-24f;
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -177,7 +178,8 @@ __device__ __forceinline__ int choose(const RouteArgs& a, const Lane<E>& w, bool
     if (sizeof(KEY) == 4 && scored) {
       const float in = rank < a.keep ? float(score) : INFINITY, out = rank < a.keep || w.g >= a.groups ? kNone : float(score);
       const float low = -group_max<GL>(-in), high = group_max<GL>(out);
-      good = high == kNone || low - high > 2.0f * (2.0f * err + 0x1p-23f * (1.0f + fabsf(low) + fabsf(high)));
+      // (two scores of a softmax add up to 1 at most, two others to 2)
+      good = high == kNone || low - high > 2.0f * (2.0f * (rel + err) + 0x1p-23f * (1.0f + fabsf(low) + fabsf(high)));
     }
     if (rank >= a.keep) {
 #pragma unroll
@@ -225,7 +227,8 @@ __device__ __forceinline__ int choose(const RouteArgs& a, const Lane<E>& w, bool
     for (int j = w.lr; j + 1 < found; j += GL) {
       const Record p = line[j], q = line[j + 1];
       const bool tie = p.l == q.l && p.b == q.b;
-      if (!tie && !(p.c - q.c > 2.0f * (err + 0x1p-23f * (1.0f + fabsf(p.c))))) good = false;
+      const float room = rel * (fabsf(p.c - p.b) + fabsf(q.c - q.b)) + 2.0f * err + 0x1p-22f * (1.0f + fabsf(p.c));
+      if (!tie && !(p.c - q.c > room)) good = false;
     }
   }
   if (sizeof(KEY) == 4 && scored) {
