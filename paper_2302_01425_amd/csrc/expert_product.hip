@@ -30,8 +30,8 @@ int64_t row_tiles(const RowsArgs& g, int64_t rows, int64_t cols) {
 //   float32: 64 x 64, bound by the matrix unit already.
 //   whole parts, 64 x 64 / 256 x 256: 2048 -> 4096, 16 experts of 8, 64, 128, 256 rows on average 37 / 41, 60 / 68, 99 / 78,
 //     170 / 116; 8 experts of 128 rows, 1024 -> 1024, 32 tiles of 256 x 256: 16 / 34; 16 of 250, 1000 -> 2008, 128 tiles 55 / 40.
-//   others, 64 x 64 / 128 x 128: 64 experts of 32 rows, 1025 -> 2047 68 / 78, of 256 278 / 225; 16 of 250, 1001 -> 2005 (512 tiles)
-//     63 / 56, 2005 -> 1001 (256 tiles) 90 / 94; 40 of 70, 777 -> 333 16 / 24.
+//   others, 64 x 64 / 128 x 128: 64 experts of 32, 64, 256 rows, 1025 -> 2047 68 / 80, 109 / 113, 284 / 215; 16 of 250, 1001 ->
+//     2005 62 / 58; 10 of 300, 515 -> 1001 (240 tiles) 20 / 18, 1001 -> 515 (150 tiles) 18 / 25; 8 of 2048, 2001 -> 3001 586 / 388.
 int launch_rows(int type, const RowsArgs& g, bool k_contiguous, hipStream_t stream) {
   if (type == kF32) return launch_rows_tiles(type, g, k_contiguous, kSmall, stream);
   const int64_t share = even_share(g.slots, g.n);
@@ -40,7 +40,7 @@ int launch_rows(int type, const RowsArgs& g, bool k_contiguous, hipStream_t stre
   const bool whole = g.limit > 0 && whole_parts(g.a, g.a_stride, g.depth, s) &&
                      whole_parts(g.w, g.w_stride, k_contiguous ? g.depth : g.cols, s) && g.w_expert * s % 16 == 0;
   if (whole && share >= 96 && row_tiles(g, 256, 256) >= 96) return launch_rows_large(type, g, k_contiguous, stream);
-  const bool middle = share >= 128 && row_tiles(g, 128, 128) >= 400;
+  const bool middle = share >= 128 && row_tiles(g, 128, 128) >= 200;
   return launch_rows_tiles(type, g, k_contiguous, middle ? kMiddle : kSmall, stream);
 }
 
@@ -71,11 +71,11 @@ int launch_product_dw(int type, const ProductArgs& p, hipStream_t stream) {
   const bool whole = whole_parts(g.a, g.a_stride, g.m, s) && whole_parts(g.b, g.b_stride, g.cols, s) &&
                      g.a_stride * s < (int64_t(1) << 32) && g.b_stride * s < (int64_t(1) << 32);   // (32-bit products of rows)
   // (bfloat16, us)  Whole parts, 64 x 64 / 128 x 256: 64 experts of 16, 64, 256 rows, 2048 x 1024 122 / 89, 159 / 106, 281 / 172; 8
-  // of 128, 1024 x 1024, 256 tiles: 19 / 20.  Others, 64 x 64 / 128 x 128: 1025 x 2047, 64 experts of 32 rows 184 / 153, of 256
-  // 375 / 347; 16 of 250 rows, 1001 x 2005, 2048 tiles 77 / 84; 8 of 8, 2047 x 2047, 2048 tiles 50 / 43; 40 of 70 rows, 777 x 333, 840
-  // tiles 23 / 30.
+  // of 128, 1024 x 1024, 256 tiles: 19 / 20.  Others, 64 x 64 / 128 x 128: 1025 x 2047, 64 experts of 32 rows 190 / 160, of 256
+  // 374 / 271; 4 of 139 rows, 1501 x 1501, 576 tiles 20 / 19; 40 of 70, 777 x 333, 840 tiles 23 / 23; 10 of 300, 515 x 1001, 400
+  // tiles 24 / 29.
   if (whole && p.n * cut(g.m, 128) * cut(g.cols, 256) >= 256) return launch_weight_tiles(type, g, kWideDirect, stream);
-  return launch_weight_tiles(type, g, p.n * cut(g.m, 128) * cut(g.cols, 128) >= 2048 ? kMiddle : kSmall, stream);
+  return launch_weight_tiles(type, g, p.n * cut(g.m, 128) * cut(g.cols, 128) >= 600 ? kMiddle : kSmall, stream);
 }
 
 }  // namespace topk

@@ -32,12 +32,9 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& g, const Found& f, cha
   const uint32_t lds0 = lds_address(lds);
   const int wave = int(threadIdx.x) / kWave;
   const int wm = (wave & 1) * (ROWS / 2), wn = (wave >> 1) * (kCols / 4);
-  constexpr int MI = ROWS / 2 / 16, NJ = kCols / 4 / 16;
-  f32x4 acc[MI][NJ];
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  constexpr int MI = ROWS / 2 / 32, NJ = kCols / 4 / 32;
+  f32x16 acc[MI][NJ];
+  clear(acc);
 
   const int steps = int((g.depth + IA::kStepK - 1) / IA::kStepK);
   int at = int(f.col * steps / g.col_tiles);               // the next step to be loaded
@@ -48,20 +45,25 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& g, const Found& f, cha
     a.issue(k0, g.depth, lds0 + stage * kStageBytes);
     b.issue(k0, g.depth, lds0 + stage * kStageBytes + kRows * kStep);
   };
-  Fragment<T> fa[2][MI], fb[2][NJ];
+  Fragment<T> fa[2][2][MI], fb[2][2][NJ];                  // of both halves of a step
   const auto read = [&](int stage, int half) {
     const char* la = lds + stage * kStageBytes;
     const char* lb = la + kRows * kStep;
 #pragma unroll
-    for (int i = 0; i < MI; ++i) fa[half][i] = IA::read(la, wm + 16 * i, half);
+    for (int t = 0; t < 2; ++t) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) fb[half][j] = IB::read(lb, wn + 16 * j, half);
+      for (int i = 0; i < MI; ++i) fa[half][t][i] = IA::read(la, wm + 32 * i, 2 * half + t);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) fb[half][t][j] = IB::read(lb, wn + 32 * j, 2 * half + t);
+    }
   };
   const auto multiply = [&](int half) {
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[i][j] = mma(0, fb[half][j], fa[half][i], acc[i][j]);
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = mma(0, fb[half][t][j], fa[half][t][i], acc[i][j]);
   };
   issue(0, 0);
   wait_stage<0>();

@@ -5,9 +5,11 @@
 // is 64 bytes of k, 24 KB of LDS for both operands, so that two workgroups share a compute unit and one multiplies while the
 // other begins, ends or waits: an expert's rows (the k of dW) are few.  For dW of whole, aligned parts, which are loaded
 // straight to LDS two steps ahead (three images).
-// Middle, 128 x 128 (steps of 64 bytes), and Small, 64 x 64 (of 128 bytes), of any alignment: operands pass through registers,
-// two steps ahead, to two images of 16 KB; three and four workgroups share a compute unit.  Small is for float32, whose matrix
-// instructions take 16 times as long for the same fragments, and where larger tiles would leave compute units without work.
+// Middle, 128 x 128 (steps of 128 bytes for rows, which are read along k, of 64 for dW), and Small, 64 x 64 (of 128 bytes), of
+// any alignment: operands pass through registers, two steps ahead, to two images; two and four workgroups share a compute
+// unit.  Small is for float32, whose matrix instructions take 16 times as long for the same fragments, and where larger tiles
+// would leave compute units without work.  What binds the others is the first cache: 16 bytes at any address take twice the
+// time of aligned ones (8192 tokens x 2, 8 experts, 2001 -> 3001, bfloat16: 388 us, without the loads 178).
 #include "expert_tiles.hpp"
 
 namespace topk {
@@ -15,46 +17,37 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// a tile of ROWS x COLS (A, B), steps of STEP bytes of k
+// a tile of ROWS x COLS (A, B), steps of STEP bytes of k, 2 x 2 wavefronts
 template <class T_, int ROWS, int COLS, int STEP>
 struct Tile {
   using T = T_;
   static constexpr int kRows = ROWS, kCols = COLS, kStep = STEP;
   static constexpr int kStageBytes = (ROWS + COLS) * STEP;
-  static constexpr int MI = ROWS / 2 / 16, NJ = COLS / 2 / 16;
+  static constexpr int MI = ROWS / 2 / 32, NJ = COLS / 2 / 32;
   template <bool KC>
   using A = Image<T, KC, ROWS, kThreads, STEP>;
   template <bool KC>
   using B = Image<T, KC, COLS, kThreads, STEP>;
-  using Sums = f32x4[MI][NJ];
+  using Sums = f32x16[MI][NJ];
   static __device__ __forceinline__ int wave_row() { return (int(threadIdx.x) / kWave & 1) * (ROWS / 2); }
   static __device__ __forceinline__ int wave_col() { return (int(threadIdx.x) / kWave >> 1) * (COLS / 2); }
 };
 template <class T>
 using Wide = Tile<T, 128, 256, 64>;
-template <class T>
-using Middle = Tile<T, 128, 128, 64>;
+template <class T, int STEP>
+using Middle = Tile<T, 128, 128, STEP>;
 template <class T>
 using Small = Tile<T, 64, 64, 128>;
-
-template <class TILE>
-__device__ __forceinline__ void clear(typename TILE::Sums& acc) {
-#pragma unroll
-  for (int i = 0; i < TILE::MI; ++i)
-#pragma unroll
-    for (int j = 0; j < TILE::NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-}
 
 template <class TILE, class IA, class IB>
 __device__ __forceinline__ void multiply(const char* stage, typename TILE::Sums& acc) {
 #pragma unroll
-  for (int half = 0; half < TILE::kStep / 64; ++half) {
+  for (int t = 0; t < TILE::kStep / 32; ++t) {
     Fragment<typename TILE::T> fa[TILE::MI], fb[TILE::NJ];
 #pragma unroll
-    for (int i = 0; i < TILE::MI; ++i) fa[i] = IA::read(stage, TILE::wave_row() + 16 * i, half);
+    for (int i = 0; i < TILE::MI; ++i) fa[i] = IA::read(stage, TILE::wave_row() + 32 * i, t);
 #pragma unroll
-    for (int j = 0; j < TILE::NJ; ++j) fb[j] = IB::read(stage + IA::kBytes, TILE::wave_col() + 16 * j, half);
-    // (the instructions that add to the same sums lie apart)
+    for (int j = 0; j < TILE::NJ; ++j) fb[j] = IB::read(stage + IA::kBytes, TILE::wave_col() + 32 * j, t);
 #pragma unroll
     for (int q = 0; q < kMma<typename TILE::T>; ++q)
 #pragma unroll
@@ -97,16 +90,15 @@ __device__ __forceinline__ void sum_staged(char* lds, LA& a, LB& b, const Table&
   constexpr bool kApart = sizeof(typename TILE::T) == 4;
   typename TILE::Sums part;
   typename TILE::Sums& acc = kApart ? part : sums;
-  if constexpr (kApart) clear<TILE>(part);
+  if constexpr (kApart) clear(part);
   const auto add_part = [&]() {
 #pragma unroll
     for (int i = 0; i < TILE::MI; ++i)
 #pragma unroll
       for (int j = 0; j < TILE::NJ; ++j) sums[i][j] += part[i][j];
-    clear<TILE>(part);
+    clear(part);
   };
   const auto load = [&](int set, int64_t k0) {
-    if (k0 >= depth) return;
     if constexpr (LISTED) {
       if ((k0 & (kTable - 1)) == 0) table.fill<kThreads>(k0, depth);
     }
@@ -119,11 +111,11 @@ __device__ __forceinline__ void sum_staged(char* lds, LA& a, LB& b, const Table&
 #pragma unroll
     for (int set = 0; set < 2; ++set) {
       const int64_t k = k0 + set * IA::kStepK;
-      if (k >= depth) break;
+      if (set == 1 && k >= depth) break;
       // (the image that is written was read two steps ago, and a barrier lies between)
       char* image = lds + set * TILE::kStageBytes;
-      a.store(set, image);
-      b.store(set, image + IA::kBytes);
+      a.store(set, image, k, depth);
+      b.store(set, image + IA::kBytes, k, depth);
       __syncthreads();
       load(set, k + 2 * IA::kStepK);
       multiply<TILE, IA, IB>(image, acc);
@@ -133,7 +125,13 @@ __device__ __forceinline__ void sum_staged(char* lds, LA& a, LB& b, const Table&
   if constexpr (kApart) add_part();
 }
 
-template <class TILE, bool B_KC>
+// First column (row) of tile number `tile` of `end`, `size` each.  The last one ends where the operand ends, and computes again,
+// alike, what it shares with the one before: no part of it crosses the end.
+__device__ __forceinline__ int64_t tile_start(int64_t tile, int64_t size, int64_t end) {
+  return min(tile * size, max(end - size, int64_t(0)));
+}
+
+template <class TILE, bool B_KC, bool TINY>
 __global__ __launch_bounds__(kThreads, 2) void rows_tiles_kernel(RowsArgs g) {
   using T = typename TILE::T;
   __shared__ __attribute__((aligned(1024))) char lds[2 * TILE::kStageBytes];
@@ -141,94 +139,108 @@ __global__ __launch_bounds__(kThreads, 2) void rows_tiles_kernel(RowsArgs g) {
   if (!find_tile<kThreads>(g.offset, g.n, g.slots, blockIdx.x, g.col_tiles, TILE::kRows, &f)) return;
   using IA = typename TILE::template A<true>;
   using IB = typename TILE::template B<B_KC>;
-  const int64_t n0 = f.col * TILE::kCols;
+  const int64_t n0 = tile_start(f.col, TILE::kCols, g.cols);
   const T* w = static_cast<const T*>(g.w) + f.expert * g.w_expert;
-  Staged<IA, false> a;
+  Staged<IA, false, TINY> a;
   a.init_rows(g.a, g.a_stride, g.source, g.div, g.limit, f.begin, f.end);
-  Staged<IB, false> b;
+  Staged<IB, false, TINY> b;
   if constexpr (B_KC) b.init_rows(w, g.w_stride, nullptr, Divisor{}, 0, n0, g.cols);
   else b.init_columns(w, g.w_stride, nullptr, n0, g.cols, 0);
   typename TILE::Sums acc;
-  clear<TILE>(acc);
+  clear(acc);
   sum_staged<TILE, IA, IB, false>(lds, a, b, Table{}, g.depth, acc);
   store_tile(acc, f.begin + TILE::wave_row(), f.end, n0 + TILE::wave_col(), g.cols, nullptr, Divisor{}, 0, static_cast<T*>(g.c),
              g.cols);
 }
 
 // LIST: which operand's rows are found through source (0: neither, 1: A, 2: B)
-template <class TILE, int LIST, bool DIRECT>
+enum Load { kDirect, kStaged, kTiny };
+template <class TILE, int LIST, Load LOAD>
 __global__ __launch_bounds__(kThreads, 2) void weight_tiles_kernel(WeightArgs g) {
   using T = typename TILE::T;
-  __shared__ __attribute__((aligned(1024))) char lds[(DIRECT ? 3 : 2) * TILE::kStageBytes];
+  __shared__ __attribute__((aligned(1024))) char lds[(LOAD == kDirect ? 3 : 2) * TILE::kStageBytes];
   __shared__ int32_t rows[LIST != 0 ? kTable : 1];
   int e;
   int64_t tile;
   if (!die_share(blockIdx.x, g.m_tiles * g.col_tiles, &e, &tile)) return;
   int64_t begin, end;
   places(g.offset, e, g.slots, &begin, &end);
-  const int64_t m0 = tile / g.col_tiles * TILE::kRows, n0 = tile % g.col_tiles * TILE::kCols;
+  int64_t m0 = tile / g.col_tiles * TILE::kRows, n0 = tile % g.col_tiles * TILE::kCols;
+  if constexpr (LOAD != kDirect) {
+    m0 = tile_start(tile / g.col_tiles, TILE::kRows, g.m);
+    n0 = tile_start(tile % g.col_tiles, TILE::kCols, g.cols);
+  }
   using IA = typename TILE::template A<false>;
   using IB = typename TILE::template B<false>;
-  std::conditional_t<DIRECT, Direct<IA, LIST == 1>, Staged<IA, LIST == 1>> a;
+  std::conditional_t<LOAD == kDirect, Direct<IA, LIST == 1>, Staged<IA, LIST == 1, LOAD == kTiny>> a;
   a.init_columns(g.a, g.a_stride, rows, m0, g.m, begin);
-  std::conditional_t<DIRECT, Direct<IB, LIST == 2>, Staged<IB, LIST == 2>> b;
+  std::conditional_t<LOAD == kDirect, Direct<IB, LIST == 2>, Staged<IB, LIST == 2, LOAD == kTiny>> b;
   b.init_columns(g.b, g.b_stride, rows, n0, g.cols, begin);
   typename TILE::Sums acc;
-  clear<TILE>(acc);
+  clear(acc);
   if (begin < end) {
     const Table table{rows, LIST == 0 ? nullptr : (LIST == 1 ? g.a_source : g.b_source) + begin, g.div,
                       LIST == 1 ? g.a_limit : g.b_limit};
-    if constexpr (DIRECT) sum_direct<TILE, IA, IB, LIST != 0>(lds, a, b, table, end - begin, acc);
+    if constexpr (LOAD == kDirect) sum_direct<TILE, IA, IB, LIST != 0>(lds, a, b, table, end - begin, acc);
     else sum_staged<TILE, IA, IB, LIST != 0>(lds, a, b, table, end - begin, acc);
   }
   store_tile(acc, m0 + TILE::wave_row(), g.m, n0 + TILE::wave_col(), g.cols, nullptr, Divisor{}, 0,
              static_cast<T*>(g.c) + e * g.m * g.cols, g.cols);
 }
 
-template <class TILE>
+template <class TILE, bool TINY>
 int rows_tile(RowsArgs g, bool k_contiguous, hipStream_t stream) {
   g.col_tiles = (g.cols + TILE::kCols - 1) / TILE::kCols;
   const int64_t blocks = rows_blocks(g, TILE::kRows);
   if (blocks >= (int64_t(1) << 31)) return -1;
   const dim3 grid = dim3(unsigned(blocks)), block(kThreads);
-  if (k_contiguous) hipLaunchKernelGGL((rows_tiles_kernel<TILE, true>), grid, block, 0, stream, g);
-  else hipLaunchKernelGGL((rows_tiles_kernel<TILE, false>), grid, block, 0, stream, g);
+  if (k_contiguous) hipLaunchKernelGGL((rows_tiles_kernel<TILE, true, TINY>), grid, block, 0, stream, g);
+  else hipLaunchKernelGGL((rows_tiles_kernel<TILE, false, TINY>), grid, block, 0, stream, g);
   return 0;
 }
 
-template <class TILE, bool DIRECT>
+template <class TILE, Load LOAD>
 int weight_tile(WeightArgs g, hipStream_t stream) {
   g.m_tiles = (g.m + TILE::kRows - 1) / TILE::kRows;
   g.col_tiles = (g.cols + TILE::kCols - 1) / TILE::kCols;
   const int64_t blocks = g.n * ((g.m_tiles * g.col_tiles + kDies - 1) / kDies) * kDies;
   if (blocks >= (int64_t(1) << 31)) return -1;
   const dim3 grid = dim3(unsigned(blocks)), block(kThreads);
-  if (g.a_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 1, DIRECT>), grid, block, 0, stream, g);
-  else if (g.b_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 2, DIRECT>), grid, block, 0, stream, g);
-  else hipLaunchKernelGGL((weight_tiles_kernel<TILE, 0, DIRECT>), grid, block, 0, stream, g);
+  if (g.a_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 1, LOAD>), grid, block, 0, stream, g);
+  else if (g.b_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 2, LOAD>), grid, block, 0, stream, g);
+  else hipLaunchKernelGGL((weight_tiles_kernel<TILE, 0, LOAD>), grid, block, 0, stream, g);
   return 0;
 }
 template <class T>
-int rows_type(const RowsArgs& g, bool k_contiguous, bool middle, hipStream_t stream) {
-  return middle ? rows_tile<Middle<T>>(g, k_contiguous, stream) : rows_tile<Small<T>>(g, k_contiguous, stream);
+int rows_type(const RowsArgs& g, bool k_contiguous, TileKind kind, hipStream_t stream) {
+  // rows shorter than 16 bytes
+  if (g.depth < 16 / int(sizeof(T)) || (!k_contiguous && g.cols < 16 / int(sizeof(T))))
+    return rows_tile<Small<T>, true>(g, k_contiguous, stream);
+  if constexpr (sizeof(T) == 2)
+    if (kind == kMiddle) return rows_tile<Middle<T, 128>, false>(g, k_contiguous, stream);
+  return rows_tile<Small<T>, false>(g, k_contiguous, stream);
 }
 template <class T>
 int weight_type(const WeightArgs& g, TileKind kind, hipStream_t stream) {
-  if (kind == kWideDirect) return weight_tile<Wide<T>, true>(g, stream);
-  return kind == kMiddle ? weight_tile<Middle<T>, false>(g, stream) : weight_tile<Small<T>, false>(g, stream);
+  if (g.m < 16 / int(sizeof(T)) || g.cols < 16 / int(sizeof(T))) return weight_tile<Small<T>, kTiny>(g, stream);
+  if constexpr (sizeof(T) == 2) {
+    if (kind == kWideDirect) return weight_tile<Wide<T>, kDirect>(g, stream);
+    if (kind == kMiddle) return weight_tile<Middle<T, 64>, kStaged>(g, stream);
+  }
+  return weight_tile<Small<T>, kStaged>(g, stream);
 }
 
 }  // namespace
 
 int launch_rows_tiles(int type, const RowsArgs& g, bool k_contiguous, TileKind kind, hipStream_t stream) {
-  if (type == kF32) return rows_tile<Small<float>>(g, k_contiguous, stream);
-  if (type == kBF16) return rows_type<bf16>(g, k_contiguous, kind == kMiddle, stream);
-  if (type == kF16) return rows_type<f16>(g, k_contiguous, kind == kMiddle, stream);
+  if (type == kF32) return rows_type<float>(g, k_contiguous, kind, stream);
+  if (type == kBF16) return rows_type<bf16>(g, k_contiguous, kind, stream);
+  if (type == kF16) return rows_type<f16>(g, k_contiguous, kind, stream);
   return -1;
 }
 
 int launch_weight_tiles(int type, const WeightArgs& g, TileKind kind, hipStream_t stream) {
-  if (type == kF32) return weight_tile<Small<float>, false>(g, stream);
+  if (type == kF32) return weight_type<float>(g, kind, stream);
   if (type == kBF16) return weight_type<bf16>(g, kind, stream);
   if (type == kF16) return weight_type<f16>(g, kind, stream);
   return -1;

@@ -11,12 +11,11 @@ __device__ const uint4 zero_part = {0, 0, 0, 0};     // read in the place of wha
 // LDS image of one step (STEP bytes of k) of an operand's R rows, cut into 16-byte parts.
 // KC, the operand is contiguous in k: an image row is a row of the operand.  Parts of a row change places, so that a quarter of
 // a 16-byte read (lanes 0..3, 12..15, 20..27; then 4..11, 16..19, 28..31; and so on) meets 16 different bank groups: part p of
-// row r lies at p ^ (r / 2 % 8) with rows of 128 bytes, at p ^ 3 (r / 8 % 2) with rows of 64 (p ^ (r / 4 % 4) leaves
-// conflicts of two).
+// row r lies at p ^ (r / 2 % 8) with rows of 128 bytes, at p ^ (r / 4 % 4) with rows of 64.
 // Else an image row is one k of all R.  16-bit types are read transposed (a quarter of a wavefront reads 4 rows of 16 elements
-// and gets 4 k of one column per lane); blocks of 32 bytes change places by k % 4 and k / 8 % 2, which the eight rows read
-// at a time differ in (rows of 128 bytes: by k / 2 % 2 and k / 8 % 2, odd and even ones lie in different banks anyway).  float32
-// is read element by element; blocks of 64 bytes change places by k / 4.
+// and gets 4 k of one column per lane); half a wavefront reads 64 bytes of four rows, so blocks of 64 bytes change places by
+// k % 4 (rows of 128 bytes: by k / 2 % 2, odd and even ones lie in different banks anyway).  float32 is read element by
+// element, 128 bytes of two rows that are four apart; blocks of 128 bytes change places by k / 4 % 2.
 template <class T, bool KC, int R, int THREADS, int STEP>
 struct Image {
   using Type = T;
@@ -27,35 +26,33 @@ struct Image {
   static constexpr int kParts = kBytes / 16 / THREADS;   // per thread
   static constexpr int kStepK = STEP / int(sizeof(T));
   static constexpr int kAlong = KC ? STEP / 16 : R / N;  // parts of an image row
+  static_assert(R >= 64 && (STEP == 64 || STEP == 128), "exchanges stay inside a row");
 
-  // Exchange of image row r, in blocks of 32 bytes (16-bit types): stays below the blocks of a row.
+  // what the number of a part in image row r is changed by
   static __device__ __forceinline__ int exchange(int r) {
-    static_assert(KC || sizeof(T) == 4 || R == 64 || R >= 128, "rows of four blocks, or of eight at least");
-    static_assert(KC || sizeof(T) == 2 || R >= 64, "rows of four blocks of 64 bytes at least");
-    if constexpr (R == 64) return ((r >> 1) & 1) | ((r >> 3) & 1) << 1;
-    else return (r & 3) | ((r >> 3) & 1) << 2;
+    if constexpr (KC && STEP == 128) return (r >> 1) & 7;
+    else if constexpr (KC) return (r >> 2) & 3;
+    else if constexpr (sizeof(T) == 4) return ((r >> 2) & 1) << 3;
+    else if constexpr (R == 64) return ((r >> 1) & 1) << 2;
+    else return (r & 3) << 2;
   }
   // the thread's part i lies at 16 (i THREADS + thread); its image row, and which part of the operand's row it is
   static __device__ __forceinline__ int row_of(int i) { return (i * THREADS + int(threadIdx.x)) / kAlong; }
   static __device__ __forceinline__ int part_of(int i) {
-    const int c = (i * THREADS + int(threadIdx.x)) % kAlong, r = row_of(i);
-    if constexpr (KC && STEP == 128) return c ^ ((r >> 1) & 7);
-    else if constexpr (KC) return c ^ ((r >> 3) & 1) * 3;
-    else if constexpr (sizeof(T) == 2) return c ^ exchange(r) << 1;
-    else return c ^ (((r >> 2) & 3) << 2);
+    return (i * THREADS + int(threadIdx.x)) % kAlong ^ exchange(row_of(i));
   }
 
-  // 16 bytes of k, out of the 64 from 64 * half on, of row lane % 16 of the 16 rows from r0 (a multiple of 16)
-  static __device__ __forceinline__ Fragment<T> read(const char* lds, int r0, int half) {
-    const int lane = int(threadIdx.x) & (kWave - 1), g = lane >> 4, l = lane & 15;
+  // 16 bytes of k of row lane % 32 of the 32 rows from r0 (a multiple of 32): those of lane / 32 in the 32 bytes from 32 t on
+  static __device__ __forceinline__ Fragment<T> read(const char* lds, int r0, int t) {
+    const int lane = int(threadIdx.x) & (kWave - 1), h = lane >> 5, l = lane & 31;
     if constexpr (KC) {
-      const int part = STEP == 128 ? (half * 4 + g) ^ (l >> 1) : g ^ (l >> 3) * 3;
-      return *reinterpret_cast<const Fragment<T>*>(lds + (r0 + l) * STEP + (part << 4));
+      return *reinterpret_cast<const Fragment<T>*>(lds + (r0 + l) * STEP + (((2 * t + h) ^ exchange(l)) << 4));
     } else if constexpr (sizeof(T) == 2) {
       typedef short s4 __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) s4* Lds4;
-      const int row = half * 32 + 8 * g + (l >> 2);        // (row + 4 has the same exchange)
-      const char* at = lds + row * (R * 2) + (((r0 >> 4) ^ exchange(row)) << 5) + (l & 3) * 8;
+      const int q = lane & 15, row = 16 * t + 8 * h + (q >> 2);          // (row + 4 has the same exchange)
+      const int part = ((r0 >> 3) + ((lane >> 4) & 1) * 2 + ((q >> 1) & 1)) ^ exchange(row);
+      const char* at = lds + row * (R * 2) + (part << 4) + (q & 1) * 8;
       union {
         s4 half[2];
         Fragment<T> whole;
@@ -64,7 +61,8 @@ struct Image {
       u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(at + 4 * R * 2));
       return u.whole;
     } else {
-      const char* at = lds + (half * 16 + 4 * g) * (R * 4) + (((r0 >> 4) ^ g) << 6) + l * 4;
+      const int row = 8 * t + 4 * h;                                     // (the same exchange for four rows)
+      const char* at = lds + row * (R * 4) + ((((r0 + l) >> 2) ^ exchange(row)) << 4) + (l & 3) * 4;
       Fragment<T> v;
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const float*>(at + j * R * 4);
@@ -164,16 +162,19 @@ struct Direct {
   }
 };
 
-// An operand of any alignment and width, loaded to one of two sets of registers and written to LDS two steps later.
-template <class IMAGE, bool LISTED>
+// An operand of any alignment and width, loaded to one of two sets of registers and written to LDS two steps later.  Every load
+// is one of 16 bytes, and every step has as many, so that the waits count exactly: a part that crosses the end of its row is
+// read from N elements before the end and shifted into place when it is written.  TINY: rows shorter than that, element by
+// element.
+template <class IMAGE, bool LISTED, bool TINY>
 struct Staged {
   using T = typename IMAGE::Type;
   static constexpr bool KC = IMAGE::kKC;
   static constexpr int N = IMAGE::N;
-  const T* p[IMAGE::kParts];       // as in Direct; null: a row (a column) of zeros
+  const T* p[IMAGE::kParts];       // as in Direct; null (KC): a row of zeros
   int64_t stride;                  // elements
   const int32_t* table;
-  int64_t edge;                    // not KC: columns from the operand's start to its end, seen from column 0 of the tile
+  int64_t edge;                    // not KC: columns from the tile's first to the operand's end
   Fragment<T> v[2][IMAGE::kParts];
 
   __device__ __forceinline__ void init_rows(const void* base, int64_t row_stride, const int32_t* source, const Divisor& d,
@@ -197,95 +198,116 @@ struct Staged {
     edge = end - first;
 #pragma unroll
     for (int i = 0; i < IMAGE::kParts; ++i) {
-      p[i] = static_cast<const T*>(base) + first + IMAGE::part_of(i) * N;
+      // (columns behind the end are not stored)
+      p[i] = static_cast<const T*>(base) + first + (TINY ? IMAGE::part_of(i) * N : min(int64_t(IMAGE::part_of(i) * N), edge - N));
       if (!LISTED) p[i] += (k_begin + IMAGE::row_of(i)) * stride;
     }
   }
 
-  // the first `count` elements at `from`, zeros behind them
-  static __device__ __forceinline__ Fragment<T> some(const T* from, int64_t count) {
-    Fragment<T> q;
-#pragma unroll
-    for (int j = 0; j < N; ++j) q[j] = j < count ? from[j] : T(0.0f);
-    return q;
+  // how far part i, read in step k0, lies before its place
+  __device__ __forceinline__ int behind(int i, int64_t k0, int64_t depth) const {
+    const int64_t over = (KC ? k0 : int64_t(0)) + IMAGE::part_of(i) * N + N - (KC ? depth : edge);
+    return int(min(max(over, int64_t(0)), int64_t(N)));
+  }
+  // elements d .. of q, zeros behind them
+  static __device__ __forceinline__ Fragment<T> shifted(const Fragment<T>& q, int d) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    u32x4 w = __builtin_bit_cast(u32x4, q);
+    const int bytes = d * int(sizeof(T));
+    if (bytes & 8) w = u32x4{w[2], w[3], 0u, 0u};
+    if (bytes & 4) w = u32x4{w[1], w[2], w[3], 0u};
+    if (bytes & 2) w = u32x4{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
+    return __builtin_bit_cast(Fragment<T>, w);
   }
   static __device__ __forceinline__ Fragment<T> whole(const T* from) {
     const Packed<T, N> q = load_packed<T, N>(from);
-    Fragment<T> r;
-#pragma unroll
-    for (int j = 0; j < N; ++j) r[j] = q.v[j];
-    return r;
+    return __builtin_bit_cast(Fragment<T>, q);
   }
 
   // the step k0 .. to the registers `set`, zeros from `depth` on
   __device__ __forceinline__ void load(int set, int64_t k0, int64_t depth) {
-    constexpr int kWide = KC ? 0 : IMAGE::kAlong * N;      // columns of the tile
     const T* zeros = reinterpret_cast<const T*>(&zero_part);
-    const T* from[IMAGE::kParts];
 #pragma unroll
     for (int i = 0; i < IMAGE::kParts; ++i) {
+      const T* from;
+      bool there;
       if constexpr (KC) {
-        from[i] = p[i] != nullptr ? p[i] + k0 : nullptr;
+        there = p[i] != nullptr;
+        from = p[i] + k0;
       } else if constexpr (LISTED) {
         const int row = table[(int(k0) + IMAGE::row_of(i)) & (kTable - 1)];
-        from[i] = row >= 0 ? p[i] + row * stride : nullptr;
+        there = row >= 0;
+        from = p[i] + row * stride;
       } else {
-        from[i] = p[i] + k0 * stride;
+        there = k0 + IMAGE::row_of(i) < depth;
+        from = p[i] + k0 * stride;
       }
-    }
-    if (k0 + IMAGE::kStepK <= depth && (KC || edge >= kWide)) {
+      if constexpr (TINY) {
+        const int64_t count = KC ? depth - (k0 + IMAGE::part_of(i) * N) : edge - IMAGE::part_of(i) * N;
 #pragma unroll
-      for (int i = 0; i < IMAGE::kParts; ++i) v[set][i] = whole(from[i] != nullptr ? from[i] : zeros);
-    } else {
-#pragma unroll
-      for (int i = 0; i < IMAGE::kParts; ++i) {
-        int64_t count = from[i] != nullptr ? N : 0;
+        for (int j = 0; j < N; ++j) v[set][i][j] = there && j < count ? from[j] : T(0.0f);
+      } else {
         if constexpr (KC) {
-          count = min(count, depth - (k0 + IMAGE::part_of(i) * N));
-        } else {
-          count = min(count, edge - IMAGE::part_of(i) * N);
-          if (k0 + IMAGE::row_of(i) >= depth) count = 0;
+          const int d = behind(i, k0, depth);
+          there = there && d < N;
+          from -= d;
         }
-        if (count >= N) v[set][i] = whole(from[i]);
-        else v[set][i] = some(from[i], count);
+        v[set][i] = whole(there ? from : zeros);
       }
     }
   }
-  __device__ __forceinline__ void store(int set, char* to) const {
+  __device__ __forceinline__ void store(int set, char* to, int64_t k0, int64_t depth) const {
+    const bool cross = !TINY && (KC ? k0 + IMAGE::kStepK > depth : edge < IMAGE::kAlong * N);
 #pragma unroll
-    for (int i = 0; i < IMAGE::kParts; ++i)
-      *reinterpret_cast<Fragment<T>*>(to + (i * IMAGE::kThreads + int(threadIdx.x)) * 16) = v[set][i];
+    for (int i = 0; i < IMAGE::kParts; ++i) {
+      Fragment<T> q = v[set][i];
+      if (cross) q = shifted(q, behind(i, k0, depth));
+      *reinterpret_cast<Fragment<T>*>(to + (i * IMAGE::kThreads + int(threadIdx.x)) * 16) = q;
+    }
   }
 };
 
-// Sums of a wavefront to C: MI x NJ blocks of 16 x 16 from (m0, n0) on, below (m_end, n_end).  Lane l has row l % 16 of a block
-// and four neighbouring columns (n runs along the rows of the instruction's output).  Rows whose place has no source are zeros.
+// Sums of a wavefront to C: MI x NJ blocks of 32 x 32 from (m0, n0) on, below (m_end, n_end); n runs along the rows of the
+// instruction's output, so that a lane has four neighbouring columns at a time.  Rows whose place has no source are zeros.
 template <class T, int MI, int NJ>
-__device__ __forceinline__ void store_tile(const f32x4 (&acc)[MI][NJ], int64_t m0, int64_t m_end, int64_t n0, int64_t n_end,
+__device__ __forceinline__ void store_tile(const f32x16 (&acc)[MI][NJ], int64_t m0, int64_t m_end, int64_t n0, int64_t n_end,
                                            const int32_t* source, const Divisor& div, int64_t limit, T* c, int64_t c_stride) {
   const int lane = int(threadIdx.x) & (kWave - 1);
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
-    const int64_t m = m0 + 16 * i + (lane & 15);
+    const int64_t m = m0 + 32 * i + (lane & 31);
     if (m >= m_end) continue;
     bool there = true;
     if (source != nullptr) there = source[m] >= 0 && quotient(source[m], div) < limit;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int64_t n = n0 + 16 * j + (lane >> 4) * 4;
-      T* to = c + m * c_stride + n;
-      if (n + 4 <= n_end) {
-        Packed<T, 4> q;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) q.v[r] = from_f32<T>(there ? acc[i][j][r] : 0.0f);
-        store_packed<T, 4>(to, q);
-      } else {
+      for (int q = 0; q < 4; ++q) {
+        const int64_t n = n0 + 32 * j + 8 * q + (lane >> 5) * 4;
+        T* to = c + m * c_stride + n;
+        if (n + 4 <= n_end) {
+          Packed<T, 4> v;
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (n + r < n_end) to[r] = from_f32<T>(there ? acc[i][j][r] : 0.0f);
+          for (int r = 0; r < 4; ++r) v.v[r] = from_f32<T>(there ? acc[i][j][4 * q + r] : 0.0f);
+          store_packed<T, 4>(to, v);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (n + r < n_end) to[r] = from_f32<T>(there ? acc[i][j][4 * q + r] : 0.0f);
+        }
       }
     }
   }
+}
+
+template <int MI, int NJ>
+__device__ __forceinline__ void clear(f32x16 (&acc)[MI][NJ]) {
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 }
 
 }  // namespace topk

@@ -127,7 +127,9 @@ struct __attribute__((packed, aligned(2))) Loose {
 };
 template <class T, int N>
 __device__ __forceinline__ Packed<T, N> load_packed(const T* p) {
-  return __builtin_bit_cast(Packed<T, N>, reinterpret_cast<const Loose<T, N>*>(p)->bits);
+  // (global memory, which the compiler does not see through a choice of pointers)
+  typedef const __attribute__((address_space(1))) Loose<T, N>* Global;
+  return __builtin_bit_cast(Packed<T, N>, ((Global)(uintptr_t)p)->bits);
 }
 template <class T, int N>
 __device__ __forceinline__ void store_packed(T* p, const Packed<T, N>& v) {

@@ -201,7 +201,8 @@ def test_places(gpu, rows, k, n, kind):
 PRODUCTS = [  # rows, k, n, h, ho
     (1, 1, 1, 1, 1), (1, 2, 4, 16, 8), (5, 2, 3, 33, 17), (40, 2, 4, 64, 64), (64, 2, 2, 128, 128), (70, 3, 5, 100, 260),
     (300, 1, 2, 136, 72), (130, 2, 1, 31, 129), (9, 4, 40, 256, 128), (260, 2, 3, 72, 264),
-    (700, 2, 3, 328, 520)]
+    (700, 2, 3, 328, 520), (20, 2, 3, 9, 15), (25, 1, 2, 8, 8), (50, 2, 2, 13, 67), (33, 2, 3, 23, 71), (150, 2, 2, 135, 193),
+    (90, 1, 2, 4, 5), (60, 2, 3, 70, 3)]
 
 
 def product_case(rows, k, n, h, ho, dtype, gather, wide, seed):
@@ -251,6 +252,40 @@ def test_products(gpu, rows, k, n, h, ho, dtype):
                 assert none is None and torch.equal(only[:end], dx[:end])
                 none, only = gpu.topk_expert_product_vjp(xd, wd, od, td, source=sd, k=k, want_x=False)
                 assert none is None and torch.equal(only, dw)
+
+
+@pytest.mark.parametrize("rows,k,n,h,ho", [(1500, 2, 24, 1032, 1040), (1500, 2, 24, 1033, 1047), (1500, 2, 24, 1034, 1042),
+                                           (2100, 1, 6, 2056, 2048), (700, 3, 5, 131, 1411)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+def test_large_products(gpu, rows, k, n, h, ho, dtype):
+    """Sizes of the larger tiles, experts of very different loads; the sums in float64, expert by expert."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(rows + h)
+    dt = getattr(torch, dtype)
+    liked = 1.5 * torch.randn((1, n), generator=g, device="cuda")
+    idx = (torch.randn((rows, n), generator=g, device="cuda") + liked).topk(k, dim=1).indices.to(torch.int32).contiguous()
+    idx[torch.rand(rows, generator=g, device="cuda") < 0.1] = -1
+    _, source, offset, _ = gpu.topk_expert_map(idx, n)
+    x = torch.randn((rows, h), generator=g, device="cuda").to(dt)
+    t = torch.randn((rows * k, ho), generator=g, device="cuda").to(dt)
+    w = torch.randn((n, ho, h), generator=g, device="cuda").to(dt)
+    at = offset.tolist()
+    for transposed in (False, True):
+        print("case", rows, k, n, h, ho, dtype, transposed, flush=True)
+        wd = w.transpose(1, 2).contiguous().transpose(1, 2) if transposed else w
+        out = torch.full((rows * k, ho), MARK, device="cuda", dtype=dt)
+        gpu.topk_expert_product_fwd(x, wd, offset, source=source, k=k, out=out)
+        dx = torch.full((rows * k, h), MARK, device="cuda", dtype=dt)
+        _, dw = gpu.topk_expert_product_vjp(x, wd, offset, t, source=source, k=k, dx_out=dx)
+        assert (out[at[n]:] == MARK).all() and (dx[at[n]:] == MARK).all()
+        for e in range(n):
+            part = slice(at[e], at[e + 1])
+            xe, te, we = x[(source[part] // k).long()].double(), t[part].double(), w[e].double()
+            for have, a, b, terms, name in ((out[part], xe, we.t().contiguous(), h, "out"), (dx[part], te, we, ho, "dx"),
+                                            (dw[e], te.t().contiguous(), xe, at[e + 1] - at[e], "dw")):
+                want = host(a @ b)
+                size = host(a.abs() @ b.abs())
+                within(host(have), want, (terms + 2) * 2 * U * size + HALF[dtype] * np.abs(want) + TINY[dtype], (name, e))
 
 
 def test_products_of_no_places(gpu):
