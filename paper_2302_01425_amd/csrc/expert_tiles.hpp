@@ -267,8 +267,22 @@ struct Staged {
   }
 };
 
+// N neighbouring columns from n on, those below n_end
+template <class T, int N>
+__device__ __forceinline__ void store_columns(T* row, int64_t n, int64_t n_end, const Packed<T, N>& v) {
+  if (n + N <= n_end) {
+    store_packed<T, N>(row + n, v);
+  } else {
+#pragma unroll
+    for (int r = 0; r < N; ++r)
+      if (n + r < n_end) row[n + r] = v.v[r];
+  }
+}
+
 // Sums of a wavefront to C: MI x NJ blocks of 32 x 32 from (m0, n0) on, below (m_end, n_end); n runs along the rows of the
-// instruction's output, so that a lane has four neighbouring columns at a time.  Rows whose place has no source are zeros.
+// instruction's output, so that a lane has four neighbouring columns at a time.  Of two such fours of 16-bit types, 8 columns
+// apart, lane l takes the first with that of lane l + 32 behind it, lane l + 32 the second: 16 bytes each.  Rows whose place has
+// no source are zeros.
 template <class T, int MI, int NJ>
 __device__ __forceinline__ void store_tile(const f32x16 (&acc)[MI][NJ], int64_t m0, int64_t m_end, int64_t n0, int64_t n_end,
                                            const int32_t* source, const Divisor& div, int64_t limit, T* c, int64_t c_stride) {
@@ -276,25 +290,32 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[MI][NJ], int64_t 
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     const int64_t m = m0 + 32 * i + (lane & 31);
-    if (m >= m_end) continue;
-    bool there = true;
-    if (source != nullptr) there = source[m] >= 0 && quotient(source[m], div) < limit;
+    bool there = m < m_end;
+    if (there && source != nullptr) there = source[m] >= 0 && quotient(source[m], div) < limit;
+    T* row = c + m * c_stride;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
+      Packed<T, 4> four[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t n = n0 + 32 * j + 8 * q + (lane >> 5) * 4;
-        T* to = c + m * c_stride + n;
-        if (n + 4 <= n_end) {
-          Packed<T, 4> v;
+      for (int q = 0; q < 4; ++q)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) v.v[r] = from_f32<T>(there ? acc[i][j][4 * q + r] : 0.0f);
-          store_packed<T, 4>(to, v);
-        } else {
+        for (int r = 0; r < 4; ++r) four[q].v[r] = from_f32<T>(there ? acc[i][j][4 * q + r] : 0.0f);
+      const int64_t n = n0 + 32 * j;
+      if constexpr (sizeof(T) == 2) {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (n + r < n_end) to[r] = from_f32<T>(there ? acc[i][j][4 * q + r] : 0.0f);
+        for (int q = 0; q < 4; q += 2) {
+          const u32x2 a = __builtin_bit_cast(u32x2, four[q]), b = __builtin_bit_cast(u32x2, four[q + 1]);
+          const auto x = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false);
+          const auto y = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
+          typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+          const u32x4 w = {x[0], y[0], x[1], y[1]};
+          if (m < m_end) store_columns<T, 8>(row, n + 8 * (q + (lane >> 5)), n_end, __builtin_bit_cast(Packed<T, 8>, w));
         }
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (m < m_end) store_columns<T, 4>(row, n + 8 * q + 4 * (lane >> 5), n_end, four[q]);
       }
     }
   }
