@@ -3,8 +3,14 @@
 //
 // A workgroup of eight wavefronts holds the tile's float32 sums in registers, 128 x 64 per wavefront: 12 fragments of 1 KB read
 // from LDS feed 32 matrix instructions.  A step is 128 bytes of k (whole cache lines of rows that are contiguous in k), 64 KB
-// of LDS for both operands, and lies in two halves: the fragments of a half are read while the other half is multiplied.  The
-// last tile of an expert's rows is one of 128 rows where it has no more.
+// of LDS for both operands, and lies in two halves: the fragments of a half are read while the other half is multiplied, and
+// the loads of the step after the next are issued one by one between the second half's instructions (in a run before them:
+// 354 us for 327 below).  The last tile of an expert's rows is one of 128 rows where it has no more.
+//
+// Bound by the loads of a step and the instructions beside the matrix ones, not by LDS (no bank conflicts; at 8192 tokens x 2,
+// 2 experts, 2048 -> 4096 the matrix units are busy half of the time, the wavefronts wait for loads a third).  bfloat16: one expert of
+// 8192 rows, 8192 -> 8192: 955 us, 1.15 PFLOP/s; 8192 tokens x 2 to 8 experts of unequal shares, 2048 -> 4096: 327 us forward,
+// 324 us dx, 0.84 PFLOP/s with a seventh of the multiplied rows empty.
 #include "expert_tiles.hpp"
 
 namespace topk {
@@ -38,46 +44,60 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& g, const Found& f, cha
 
   const int steps = int((g.depth + IA::kStepK - 1) / IA::kStepK);
   int at = int(f.col * steps / g.col_tiles);               // the next step to be loaded
-  // steps behind the last are loaded as zeros
-  const auto issue = [&](int step, int stage) {
+  // k of the next step that is loaded; steps behind the last are loaded as zeros
+  const auto next = [&](int step) {
     const int64_t k0 = int64_t(step < steps ? at : steps) * IA::kStepK;
     at = at + 1 == steps ? 0 : at + 1;
-    a.issue(k0, g.depth, lds0 + stage * kStageBytes);
-    b.issue(k0, g.depth, lds0 + stage * kStageBytes + kRows * kStep);
+    return k0;
+  };
+  constexpr int kLoads = IA::kParts + IB::kParts;
+  const auto issue = [&](int i, int64_t k0, int stage) {
+    if (i < IA::kParts) a.issue_part(i, k0, g.depth, lds0 + stage * kStageBytes);
+    else b.issue_part(i - IA::kParts, k0, g.depth, lds0 + stage * kStageBytes + kRows * kStep);
   };
   Fragment<T> fa[2][2][MI], fb[2][2][NJ];                  // of both halves of a step
-  const auto read = [&](int stage, int half) {
+  constexpr int kReads = 2 * (MI + NJ);
+  const auto read = [&](int i, int stage, int half) {
     const char* la = lds + stage * kStageBytes;
-    const char* lb = la + kRows * kStep;
+    const int t = i / (MI + NJ), r = i % (MI + NJ);
+    if (r < NJ) fb[half][t][r] = IB::read(la + kRows * kStep, wn + 32 * r, 2 * half + t);
+    else fa[half][t][r - NJ] = IA::read(la, wm + 32 * (r - NJ), 2 * half + t);
+  };
+  // a half multiplied; between the instructions the fragments of another half are read, and a step is loaded
+  constexpr int kTurns = MI * NJ;
+  const auto multiply = [&](int half, int stage, int other, bool load, int64_t k0, int load_stage) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int c = 0; c < kTurns; ++c) {
 #pragma unroll
-      for (int i = 0; i < MI; ++i) fa[half][t][i] = IA::read(la, wm + 32 * i, 2 * half + t);
+      for (int q = 2 * c; q < 2 * c + 2; ++q) {
+        const int t = q / (MI * NJ), i = q / NJ % MI, j = q % NJ;
+        acc[i][j] = mma(0, fb[half][t][j], fa[half][t][i], acc[i][j]);
+      }
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) fb[half][t][j] = IB::read(lb, wn + 32 * j, 2 * half + t);
+      for (int i = c * kReads / kTurns; i < (c + 1) * kReads / kTurns; ++i) read(i, stage, other);
+      if (load) {
+#pragma unroll
+        for (int i = c * kLoads / kTurns; i < (c + 1) * kLoads / kTurns; ++i) issue(i, k0, load_stage);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
-  const auto multiply = [&](int half) {
+  int64_t k0 = next(0);
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[i][j] = mma(0, fb[half][t][j], fa[half][t][i], acc[i][j]);
-  };
-  issue(0, 0);
+  for (int i = 0; i < kLoads; ++i) issue(i, k0, 0);
   wait_stage<0>();
-  issue(1, 1);
-  read(0, 0);
+  k0 = next(1);
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) issue(i, k0, 1);
+#pragma unroll
+  for (int i = 0; i < kReads; ++i) read(i, 0, 0);
   for (int step = 0; step < steps; ++step) {
     const int stage = step & 1;
-    read(stage, 1);
-    multiply(0);
+    multiply(0, stage, 1, false, 0, 0);
     // everything of this step is in registers, and the next step is there
     wait_stage<0>();
-    issue(step + 2, stage);
-    read(stage ^ 1, 0);
-    multiply(1);
+    k0 = next(step + 2);
+    multiply(1, stage ^ 1, 0, true, k0, stage);
   }
   wait_stage<0>();           // (no load may reach LDS that is another workgroup's by then)
   store_tile(acc, f.begin + wm, f.end, n0 + wn, g.cols, g.source, g.div, g.limit, static_cast<T*>(g.c), g.cols);
