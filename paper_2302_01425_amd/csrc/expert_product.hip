@@ -62,11 +62,11 @@ int launch_product_dw(int type, const ProductArgs& p, hipStream_t stream) {
   // dW has the layout of w: its contiguous direction gives the columns
   WeightArgs g;
   if (p.w_in == 1)
-    g = {p.t, p.x, p.t_stride, p.x_stride, nullptr, p.source, divisor(p.k), p.slots, p.m, p.offset, p.slots, p.n, p.ho, p.h, 0,
-         0, p.dw};
+    g = {p.t, p.x, p.t_stride, p.x_stride, nullptr, p.source, divisor(p.k), p.slots, p.m, p.offset, p.slots, p.n, p.ho, p.h,
+         p.dw};
   else
-    g = {p.x, p.t, p.x_stride, p.t_stride, p.source, nullptr, divisor(p.k), p.m, p.slots, p.offset, p.slots, p.n, p.h, p.ho, 0,
-         0, p.dw};
+    g = {p.x, p.t, p.x_stride, p.t_stride, p.source, nullptr, divisor(p.k), p.m, p.slots, p.offset, p.slots, p.n, p.h, p.ho,
+         p.dw};
   const int s = size_of(type);
   const bool whole = whole_parts(g.a, g.a_stride, g.m, s) && whole_parts(g.b, g.b_stride, g.cols, s) &&
                      g.a_stride * s < (int64_t(1) << 32) && g.b_stride * s < (int64_t(1) << 32);   // (32-bit products of rows)

@@ -85,14 +85,6 @@ __device__ __forceinline__ int64_t dealt(int64_t b, int64_t total) {
   const int64_t die = b % kDies, i = b / kDies;
   return (i / run * kDies + die) * run + i % run;
 }
-// Tile of the `tiles` ones of every expert that workgroup b of 8 * n * ceil(tiles / 8) takes, false where there is none: every
-// die has an eighth of every expert's, since experts differ in their rows.
-__device__ __forceinline__ bool die_share(int64_t b, int64_t tiles, int* expert, int64_t* tile) {
-  const int64_t share = (tiles + kDies - 1) / kDies, i = b / kDies;
-  *expert = int(i / share);
-  *tile = b % kDies * share + i % share;
-  return *tile < tiles;
-}
 // Expert, rows and columns of a workgroup's pair, false where there is none.  All threads of the workgroup call it.
 template <int kThreads>
 __device__ __forceinline__ bool find_tile(const int32_t* offset, int n, int64_t slots, int64_t block, int64_t col_tiles, int size,
@@ -162,9 +154,47 @@ struct WeightArgs {
   const int32_t* offset;
   int64_t slots;
   int n;
-  int64_t m, cols, m_tiles, col_tiles;
+  int64_t m, cols;
   void* c;
+  // tiles, and those of a die (split_tiles)
+  int64_t m_tiles = 0, col_tiles = 0, die_m = 0, die_cols = 0;
 };
+// Every die gets an eighth of every expert's tiles, since experts differ in their rows: a rectangle of the tiles, that of 1 x 8, 2 x
+// 4, 4 x 2 or 8 x 1 such rectangles that reads least, or an eighth of the tiles in row order (die_cols 0) where rectangles would
+// leave a die more than a sixteenth above that.  Returns the number of workgroups.
+inline int64_t split_tiles(WeightArgs* g, int64_t rows, int64_t cols) {
+  g->m_tiles = (g->m + rows - 1) / rows;
+  g->col_tiles = (g->cols + cols - 1) / cols;
+  const int64_t tiles = g->m_tiles * g->col_tiles;
+  int64_t share = (tiles + kDies - 1) / kDies, best = 0;
+  g->die_m = share;
+  for (int d = 1; d <= kDies; d *= 2) {
+    const int64_t m = (g->m_tiles + d - 1) / d, c = (g->col_tiles + kDies / d - 1) / (kDies / d);
+    const int64_t read = m * rows + c * cols;
+    if (m * c * kDies * 16 > tiles * 17 || (best != 0 && read >= best)) continue;
+    best = read;
+    g->die_m = m;
+    g->die_cols = c;
+    share = m * c;
+  }
+  return g->n * share * kDies;
+}
+// Expert and tile of workgroup b, false where there is none.
+__device__ __forceinline__ bool find_weight_tile(const WeightArgs& g, int64_t b, int* expert, int64_t* m, int64_t* col) {
+  const int64_t die = b % kDies, i = b / kDies;
+  if (g.die_cols == 0) {
+    const int64_t tile = die * g.die_m + i % g.die_m;
+    *expert = int(i / g.die_m);
+    *m = tile / g.col_tiles;
+    *col = tile % g.col_tiles;
+  } else {
+    const int64_t share = g.die_m * g.die_cols, across = (g.col_tiles + g.die_cols - 1) / g.die_cols, at = i % share;
+    *expert = int(i / share);
+    *m = die / across * g.die_m + at / g.die_cols;
+    *col = die % across * g.die_cols + at % g.die_cols;
+  }
+  return *m < g.m_tiles && *col < g.col_tiles;
+}
 // workgroups for all pairs: as many tiles of rows as there can be, and room for the last runs
 inline int64_t rows_blocks(const RowsArgs& g, int size) {
   return (g.slots / size + min(int64_t(g.n), g.slots)) * g.col_tiles + kDies * kRunMost;

@@ -39,8 +39,9 @@ using Middle = Tile<T, 128, 128, STEP>;
 template <class T>
 using Small = Tile<T, 64, 64, 128>;
 
-template <class TILE, class IA, class IB>
-__device__ __forceinline__ void multiply(const char* stage, typename TILE::Sums& acc) {
+// between(turn, turns): what is done between the matrix instructions
+template <class TILE, class IA, class IB, class F>
+__device__ __forceinline__ void multiply(const char* stage, typename TILE::Sums& acc, F between) {
 #pragma unroll
   for (int t = 0; t < TILE::kStep / 32; ++t) {
     Fragment<typename TILE::T> fa[TILE::MI], fb[TILE::NJ];
@@ -51,9 +52,11 @@ __device__ __forceinline__ void multiply(const char* stage, typename TILE::Sums&
 #pragma unroll
     for (int q = 0; q < kMma<typename TILE::T>; ++q)
 #pragma unroll
-      for (int j = 0; j < TILE::NJ; ++j)
+      for (int j = 0; j < TILE::NJ; ++j) {
 #pragma unroll
         for (int i = 0; i < TILE::MI; ++i) acc[i][j] = mma(q, fb[j], fa[i], acc[i][j]);
+        between((t * kMma<typename TILE::T> + q) * TILE::NJ + j, TILE::kStep / 32 * kMma<typename TILE::T> * TILE::NJ);
+      }
   }
 }
 
@@ -63,20 +66,31 @@ __device__ __forceinline__ void sum_direct(char* lds, const LA& a, const LB& b, 
                                            typename TILE::Sums& acc) {
   constexpr int kLoads = IA::kParts + IB::kParts;
   const uint32_t lds0 = lds_address(lds);
-  const auto issue = [&](int64_t k0, int stage) {          // (steps behind the last are loaded as zeros)
+  const auto fill = [&](int64_t k0) {
     if constexpr (LISTED) {
       if ((k0 & (kTable - 1)) == 0) table.fill<kThreads>(k0, depth);
     }
-    a.issue(k0, depth, lds0 + stage * TILE::kStageBytes);
-    b.issue(k0, depth, lds0 + stage * TILE::kStageBytes + IA::kBytes);
   };
-  issue(0, 0);
-  issue(IA::kStepK, 1);
+  const auto issue = [&](int i, int64_t k0, int stage) {   // (steps behind the last are loaded as zeros)
+    if (i < IA::kParts) a.issue_part(i, k0, depth, lds0 + stage * TILE::kStageBytes);
+    else b.issue_part(i - IA::kParts, k0, depth, lds0 + stage * TILE::kStageBytes + IA::kBytes);
+  };
+#pragma unroll
+  for (int stage = 0; stage < 2; ++stage) {
+    fill(stage * IA::kStepK);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) issue(i, stage * IA::kStepK, stage);
+  }
   int stage = 0;
   for (int64_t k0 = 0; k0 < depth; k0 += IA::kStepK) {
     wait_stage<kLoads>();
-    issue(k0 + 2 * IA::kStepK, stage == 0 ? 2 : stage - 1);
-    multiply<TILE, IA, IB>(lds + stage * TILE::kStageBytes, acc);
+    fill(k0 + 2 * IA::kStepK);
+    const int other = stage == 0 ? 2 : stage - 1;
+    multiply<TILE, IA, IB>(lds + stage * TILE::kStageBytes, acc, [&](int turn, int turns) {
+#pragma unroll
+      for (int i = turn * kLoads / turns; i < (turn + 1) * kLoads / turns; ++i) issue(i, k0 + 2 * IA::kStepK, other);
+      __builtin_amdgcn_sched_barrier(0);
+    });
     stage = stage == 2 ? 0 : stage + 1;
   }
   wait_stage<0>();           // (no load may reach LDS that is another workgroup's by then)
@@ -118,7 +132,7 @@ __device__ __forceinline__ void sum_staged(char* lds, LA& a, LB& b, const Table&
       b.store(set, image + IA::kBytes, k, depth);
       __syncthreads();
       load(set, k + 2 * IA::kStepK);
-      multiply<TILE, IA, IB>(image, acc);
+      multiply<TILE, IA, IB>(image, acc, [](int, int) {});
     }
     if (kApart && (k0 & (2 * IA::kStepK)) != 0) add_part();
   }
@@ -161,15 +175,12 @@ __global__ __launch_bounds__(kThreads, 2) void weight_tiles_kernel(WeightArgs g)
   __shared__ __attribute__((aligned(1024))) char lds[(LOAD == kDirect ? 3 : 2) * TILE::kStageBytes];
   __shared__ int32_t rows[LIST != 0 ? kTable : 1];
   int e;
-  int64_t tile;
-  if (!die_share(blockIdx.x, g.m_tiles * g.col_tiles, &e, &tile)) return;
+  int64_t m0, n0;
+  if (!find_weight_tile(g, blockIdx.x, &e, &m0, &n0)) return;
   int64_t begin, end;
   places(g.offset, e, g.slots, &begin, &end);
-  int64_t m0 = tile / g.col_tiles * TILE::kRows, n0 = tile % g.col_tiles * TILE::kCols;
-  if constexpr (LOAD != kDirect) {
-    m0 = tile_start(tile / g.col_tiles, TILE::kRows, g.m);
-    n0 = tile_start(tile % g.col_tiles, TILE::kCols, g.cols);
-  }
+  m0 = LOAD == kDirect ? m0 * TILE::kRows : tile_start(m0, TILE::kRows, g.m);
+  n0 = LOAD == kDirect ? n0 * TILE::kCols : tile_start(n0, TILE::kCols, g.cols);
   using IA = typename TILE::template A<false>;
   using IB = typename TILE::template B<false>;
   std::conditional_t<LOAD == kDirect, Direct<IA, LIST == 1>, Staged<IA, LIST == 1, LOAD == kTiny>> a;
@@ -201,9 +212,7 @@ int rows_tile(RowsArgs g, bool k_contiguous, hipStream_t stream) {
 
 template <class TILE, Load LOAD>
 int weight_tile(WeightArgs g, hipStream_t stream) {
-  g.m_tiles = (g.m + TILE::kRows - 1) / TILE::kRows;
-  g.col_tiles = (g.cols + TILE::kCols - 1) / TILE::kCols;
-  const int64_t blocks = g.n * ((g.m_tiles * g.col_tiles + kDies - 1) / kDies) * kDies;
+  const int64_t blocks = split_tiles(&g, TILE::kRows, TILE::kCols);
   if (blocks >= (int64_t(1) << 31)) return -1;
   const dim3 grid = dim3(unsigned(blocks)), block(kThreads);
   if (g.a_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 1, LOAD>), grid, block, 0, stream, g);

@@ -148,17 +148,14 @@ struct Direct {
     const char* from;
     if constexpr (LISTED) {
       const int row = table[(int(k0) + IMAGE::row_of(i)) & (kTable - 1)];
-      from = row >= 0 ? p[i] + uint64_t(uint32_t(row)) * uint32_t(stride) : zeros;
+      // (the row is selected before the product: a product in one of two ways would be a branch)
+      from = (row >= 0 ? p[i] : zeros) + uint64_t(uint32_t(max(row, 0))) * uint32_t(stride);
     } else {
       from = p[i] + k0 * (KC ? int64_t(sizeof(T)) : stride);
       const int left = int(min(depth - k0, int64_t(IMAGE::kStepK)));
       from = (KC ? IMAGE::part_of(i) * IMAGE::N : IMAGE::row_of(i)) < left ? from : zeros;
     }
     load_to_lds(from, to + (i * IMAGE::kThreads + wave * kWave) * 16);
-  }
-  __device__ __forceinline__ void issue(int64_t k0, int64_t depth, uint32_t to) const {
-#pragma unroll
-    for (int i = 0; i < IMAGE::kParts; ++i) issue_part(i, k0, depth, to);
   }
 };
 
