@@ -70,8 +70,8 @@ int launch_product_dw(int type, const ProductArgs& p, hipStream_t stream) {
   const int s = size_of(type);
   const bool whole = whole_parts(g.a, g.a_stride, g.m, s) && whole_parts(g.b, g.b_stride, g.cols, s) &&
                      g.a_stride * s < (int64_t(1) << 32) && g.b_stride * s < (int64_t(1) << 32);   // (32-bit products of rows)
-  // (bfloat16, us)  Whole parts, 64 x 64 / 128 x 256: 64 experts of 16, 64, 256 rows, 2048 x 1024 122 / 89, 159 / 106, 281 / 172; 8
-  // of 128, 1024 x 1024, 256 tiles: 19 / 20.  Others, 64 x 64 / 128 x 128: 1025 x 2047, 64 experts of 32 rows 190 / 160, of 256
+  // (bfloat16, us)  Whole parts, 64 x 64 / 128 x 256: 64 experts of 16, 64, 256 rows, 2048 x 1024 122 / 54, 159 / 74, 281 / 134; 8
+  // of 128, 1024 x 1024, 256 tiles: 19 / 15.  Others, 64 x 64 / 128 x 128: 1025 x 2047, 64 experts of 32 rows 190 / 160, of 256
   // 374 / 271; 4 of 139 rows, 1501 x 1501, 576 tiles 20 / 19; 40 of 70, 777 x 333, 840 tiles 23 / 23; 10 of 300, 515 x 1001, 400
   // tiles 24 / 29.
   if (whole && p.n * cut(g.m, 128) * cut(g.cols, 256) >= 256) return launch_weight_tiles(type, g, kWideDirect, stream);

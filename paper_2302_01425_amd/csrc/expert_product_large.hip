@@ -8,9 +8,9 @@
 // 354 us for 327 below).  The last tile of an expert's rows is one of 128 rows where it has no more.
 //
 // Bound by the loads of a step and the instructions beside the matrix ones, not by LDS (no bank conflicts; at 8192 tokens x 2,
-// 2 experts, 2048 -> 4096 the matrix units are busy half of the time, the wavefronts wait for loads a third).  bfloat16: one expert of
-// 8192 rows, 8192 -> 8192: 955 us, 1.15 PFLOP/s; 8192 tokens x 2 to 8 experts of unequal shares, 2048 -> 4096: 327 us forward,
-// 324 us dx, 0.84 PFLOP/s with a seventh of the multiplied rows empty.
+// 2 experts, 2048 -> 4096 the matrix units are busy half of the time, the wavefronts wait for loads a third).  bfloat16: one
+// expert of 8192 rows, 8192 -> 8192: 955 us, 1.15 PFLOP/s; 8192 tokens x 2 to 32 experts of unequal shares, 2048 -> 4096: 330 us
+// forward, 325 us dx, 0.84 PFLOP/s with a seventh of the multiplied rows empty.
 #include "expert_tiles.hpp"
 
 namespace topk {

@@ -318,6 +318,15 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[MI][NJ], int64_t 
   }
 }
 
+// Zeros to share `part` of `parts` of the `count` elements at c, by a workgroup of THREADS.
+template <int THREADS, class T>
+__device__ __forceinline__ void store_zeros(T* c, int64_t count, int64_t part, int64_t parts) {
+  constexpr int N = 16 / int(sizeof(T));
+  const int64_t whole = count / N, end = whole * (part + 1) / parts;
+  for (int64_t i = whole * part / parts + threadIdx.x; i < end; i += THREADS) store_packed<T, N>(c + i * N, Packed<T, N>{});
+  if (part == 0 && threadIdx.x < count - whole * N) c[whole * N + threadIdx.x] = T(0.0f);
+}
+
 template <int MI, int NJ>
 __device__ __forceinline__ void clear(f32x16 (&acc)[MI][NJ]) {
 #pragma unroll

@@ -625,3 +625,33 @@ def test_native_step_and_python_agree(gpu):
                     lambda: gpu.topk_combine_vjp(y, slot, val, out, dy_out=y), lambda: gpu.topk_combine_vjp(y, slot, val, out[:5])):
             r = compare(gpu, bad)
             assert isinstance(r[0], type) and issubclass(r[0], gpu.TopkError), r
+
+
+# the zeros of an expert without places: blocks of any size, so of any alignment in memory, before and behind others
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("h,ho", [(1, 1), (3, 5), (129, 7), (131, 257), (256, 520)])
+def test_weight_gradient_of_experts_without_places(gpu, h, ho, dtype):
+    import torch
+    t = getattr(torch, dtype)
+    counts = [0, 0, 2, 0, 1, 0]
+    off = torch.tensor([0] + list(np.cumsum(counts)), dtype=torch.int32, device="cuda")
+    x = torch.randn((3, h), device="cuda").to(t)
+    ct = torch.randn((3, ho), device="cuda").to(t)
+    for transposed in (False, True):
+        w = torch.randn((6, h, ho) if transposed else (6, ho, h), device="cuda").to(t)
+        w = w.transpose(1, 2) if transposed else w
+        dw = torch.full((6, h, ho) if transposed else (6, ho, h), 7.0, device="cuda", dtype=t)
+        dw = dw.transpose(1, 2) if transposed else dw
+        _, got = gpu.topk_expert_product_vjp(x, w, off, ct, want_x=False, dw_out=dw)
+        assert got is dw
+        at = 0
+        for e, c in enumerate(counts):
+            if c == 0:
+                assert torch.all(dw[e] == 0), (e, transposed)
+            else:
+                want = ct[at:at + c].cpu().double().t() @ x[at:at + c].cpu().double()
+                # two roundings of products and one of their sum, one of the output (2^-25 for a subnormal float16)
+                room = torch.finfo(t).eps / 2 * want.abs() + 3 * 2.0 ** -24 * (ct[at:at + c].cpu().double().abs().t() @
+                                                                               x[at:at + c].cpu().double().abs())
+                assert torch.all((dw[e].cpu().double() - want).abs() <= room + 2.0 ** -24), (e, transposed)
+            at += c
