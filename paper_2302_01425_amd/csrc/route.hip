@@ -5,6 +5,11 @@
 // A logit of -inf or NaN, or a bias of -inf or NaN, takes its expert out; where fewer than k are left, idx = -1, val = 0.
 // Scores are compared as float64 would: the choice jumps where two scores cross, and two float32 scores of 16384 x 256
 // cross within their rounding a few times per call.  Logits are compared as they are.
+//
+// A row lies in the registers of 8 to 64 lanes and is read once; k rounds take the largest each.  Bound by the launch below some
+// 1000 rows (5 us a call), by instructions above: a round of 32 lanes x 8 elements is 87 of them.  16384 x 64 float32, softmax, k = 2:
+// 4.2 us, 1.0 TB/s; 8192 x 256 bfloat16, sigmoid, bias, 8 groups, k = 8: 13 us a call, 0.35 TB/s (16 lanes x 16 elements: 12 to
+// 17 us, and 2 us more for few rows).
 #include <cmath>
 
 #include "experts.hpp"
@@ -109,14 +114,56 @@ __device__ __forceinline__ double max_all(const double (&v)[E]) {
   return m;
 }
 
-// A chosen element: score, logit, bias, index.
+// A chosen element: score, bias, logit, index.
 struct Record {
-  float c, l, b;
+  float c, b, l;
   int i;
 };
+constexpr int kRecords = kChoicesMax + 2;
 
-// The k largest and the next one to line[] (LDS, k + 1 records of the row), in order; returns how many there are.  KEY float:
-// `sure` says whether float64 would choose the same.  `base`: index of the lane's first element.
+__device__ __forceinline__ double sigmoid_f64(float l) { return 1.0 / (1.0 + exp(-double(l))); }
+
+// The first m records of a row in the order of their scores in float64, which take the place of c and b.  The records are few
+// and nearly in order: one lane moves them.
+template <int GL, int E>
+__device__ __forceinline__ void settle(const RouteArgs& a, const Lane<E>& w, Record* line, int m) {
+  double z = 0.0;
+  if (a.score == kSoftmax) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) z += w.l[e] == kNone ? 0.0 : exp_below(double(w.l[e]), double(w.top));
+    z = 1.0 / group_sum_f64<GL>(z);
+  }
+  const auto score = [](const Record& r) {
+    double d;
+    __builtin_memcpy(&d, &r, sizeof(d));
+    return d;
+  };
+  for (int j = w.lr; j < m; j += GL) {
+    Record r = line[j];
+    const double s = a.score == kSoftmax ? exp_below(double(r.l), double(w.top)) * z : sigmoid_f64(r.l);
+    const double d = s + double(r.b);
+    __builtin_memcpy(&r, &d, sizeof(d));
+    line[j] = r;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (w.lr == 0) {
+    for (int j = 1; j < m; ++j) {
+      const Record r = line[j];
+      const double d = score(r);
+      int to = j;
+      for (; to > 0; --to) {
+        const Record q = line[to - 1];
+        if (score(q) > d || (score(q) == d && q.i < r.i)) break;
+        line[to] = q;
+      }
+      line[to] = r;
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// The k largest and the two next to line[] (LDS, kRecords of the row), in order; returns how many of the k there are.  KEY
+// float: `sure` says whether float64 would choose the same.  `base`: index of the lane's first element.
 template <int GL, int E, class KEY>
 __device__ __forceinline__ int choose(const RouteArgs& a, const Lane<E>& w, bool scored, int base, Record* line, bool* sure) {
   KEY key[E];
@@ -141,7 +188,7 @@ __device__ __forceinline__ int choose(const RouteArgs& a, const Lane<E>& w, bool
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        if constexpr (sizeof(KEY) == 8) key[e] = 1.0 / (1.0 + exp(-double(w.l[e])));
+        if constexpr (sizeof(KEY) == 8) key[e] = sigmoid_f64(w.l[e]);
         else key[e] = 1.0f / (1.0f + expf(-w.l[e]));
       }
       // 2 of the exponential, 1 of the sum, 2 of the quotient
@@ -202,7 +249,7 @@ __device__ __forceinline__ int choose(const RouteArgs& a, const Lane<E>& w, bool
   }
   int found = 0;
   const int lane0 = int(threadIdx.x) & (kWave - 1) & ~(GL - 1);
-  const int rounds = check ? min(a.k + 1, a.n) : a.k;
+  const int rounds = check ? min(a.k + 2, a.n) : a.k;
   for (int j = 0; j < rounds; ++j) {
     const KEY best = max_all(key);
     const KEY m = group_max<GL>(best);
@@ -220,15 +267,32 @@ __device__ __forceinline__ int choose(const RouteArgs& a, const Lane<E>& w, bool
   }
 #pragma unroll
   for (int e = 0; e < E; ++e)
-    if (place[e] >= 0) line[place[e]] = Record{float(score[e]), w.l[e], w.b[e], base + e};
+    if (place[e] >= 0) line[place[e]] = Record{float(score[e]), w.b[e], w.l[e], base + e};
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");           // (other lanes read the records)
-  if (check) {
-    // neighbours in the order closer than their errors, unless they are ties
-    for (int j = w.lr; j + 1 < found; j += GL) {
-      const Record p = line[j], q = line[j + 1];
-      const bool tie = p.l == q.l && p.b == q.b;
-      const float room = rel * (fabsf(p.c - p.b) + fabsf(q.c - q.b)) + 2.0f * err + 0x1p-22f * (1.0f + fabsf(p.c));
-      if (!tie && !(p.c - q.c > room)) good = false;
+  if constexpr (sizeof(KEY) == 4) {
+    if (check) {
+      // The first m records hold the k largest if a gap behind them is wider than the errors of any two scores (at most rel + err
+      // each) and the roundings of the sums with their biases.
+      const auto apart = [&](int j) {
+        const float p = line[j].c, q = line[j + 1].c;
+        return p - q > 2.0f * (rel + err) + 0x1p-22f * (1.0f + fabsf(p) + fabsf(q));
+      };
+      int m = found;
+      if (found > a.k) {
+        if (apart(a.k - 1)) m = a.k;
+        else if (found == a.k + 1 || apart(a.k)) m = a.k + 1;
+        else good = false;
+      }
+      // and are in order if neighbours are ties or further apart than their errors; else float64 puts them in order
+      bool ordered = true;
+      for (int j = w.lr; j + 1 < m; j += GL) {
+        const Record p = line[j], q = line[j + 1];
+        const bool tie = p.l == q.l && p.b == q.b;
+        const float room = rel * (fabsf(p.c - p.b) + fabsf(q.c - q.b)) + 2.0f * err + 0x1p-22f * (1.0f + fabsf(p.c));
+        if (!tie && !(p.c - q.c > room)) ordered = false;
+      }
+      const unsigned long long off = __ballot(!ordered) >> lane0;
+      if (good && (GL < 64 ? off & ((1ull << (GL & 63)) - 1ull) : off) != 0ull) settle<GL, E>(a, w, line, m);
     }
   }
   if (sizeof(KEY) == 4 && scored) {
@@ -242,7 +306,7 @@ __device__ __forceinline__ int choose(const RouteArgs& a, const Lane<E>& w, bool
 // GL lanes per row, E elements per lane
 template <class T, int GL, int E>
 __global__ __launch_bounds__(kThreads) void route_fwd_kernel(RouteArgs a, int lanes) {
-  __shared__ __attribute__((aligned(16))) Record lines[kThreads / GL][kChoicesMax + 1];
+  __shared__ __attribute__((aligned(16))) Record lines[kThreads / GL][kRecords];
   const int64_t row = (int64_t(blockIdx.x) * kThreads + threadIdx.x) / GL;
   if (row >= a.rows) return;                                       // (whole row groups; no barrier below)
   Lane<E> w;
@@ -262,7 +326,8 @@ __global__ __launch_bounds__(kThreads) void route_fwd_kernel(RouteArgs a, int la
   w.top = group_max<GL>(max_all(w.l));
 
   // Scores, not logits, are compared where a bias is added or scores of a group are.  Float32 decides where its errors leave no
-  // doubt, float64 elsewhere (8192 x 256 with sigmoid scores, k = 8: about one row in a thousand).
+  // doubt; else float64 puts the few records in order (8192 x 256 with sigmoid scores, k = 8: about one row in a thousand), or all
+  // the row, where it is not sure which they are.
   const bool scored = a.bias != nullptr || (a.groups > 1 && a.top == 2);
   bool sure;
   Record* line = lines[threadIdx.x / GL];

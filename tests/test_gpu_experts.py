@@ -655,3 +655,26 @@ def test_weight_gradient_of_experts_without_places(gpu, h, ho, dtype):
                                                                                x[at:at + c].cpu().double().abs())
                 assert torch.all((dw[e].cpu().double() - want).abs() <= room + 2.0 ** -24), (e, transposed)
             at += c
+
+
+# scores that float32 cannot tell apart, in runs of `run` neighbours of the order that end before, at and behind the k-th place
+@pytest.mark.parametrize("n,k", [(6, 5), (40, 5), (64, 64), (200, 9), (1000, 64)])
+@pytest.mark.parametrize("run", [1, 2, 3, 4, 1000])
+def test_route_of_scores_that_cross_in_float32(gpu, n, k, run):
+    r = np.random.default_rng(n + run)
+    for sigmoid in (False, True):
+        l = r.normal(size=(24, n)).astype(np.float32)
+        l[1:] = l[0]                                        # neighbours differ by roundings of the logits and the bias
+        for row in range(1, 24):
+            at = r.integers(0, n, size=3)
+            l[row, at] = np.nextafter(l[row, at], np.float32(9.0) * (-1) ** row)
+        for start in range(min(run, 5)):
+            rank = np.empty(n, np.int64)
+            rank[r.permutation(n)] = (np.arange(n) + start) // run
+            bias = (0.9 - 0.01 * rank - ref.scores(l[:1], sigmoid)[0]).astype(np.float32)
+            want = ref.route(l, k, sigmoid, bias)[0]
+            idx, _ = gpu.topk_route_fwd(put(l), k, int(sigmoid), bias=put(bias))
+            assert np.array_equal(host(idx), want), (sigmoid, start)
+        ties = np.round(l * 4) / 4
+        idx, _ = gpu.topk_route_fwd(put(ties), k, int(sigmoid), bias=put(np.zeros(n)))
+        assert np.array_equal(host(idx), ref.route(ties, k, sigmoid, np.zeros(n))[0]), "ties"
