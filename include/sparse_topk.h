@@ -404,7 +404,7 @@ int topk_expert_product_vjp(const void* x, int64_t x_stride, int64_t m, const vo
 
 /*
  * Weighted sum per token: out[t] = sum_j val[t][j] y[slot[t][j]] (val NULL: ones), places out of [0, slots) left out.
- *   y [slots][h] of `type`, y_stride between rows; slot, val [rows][k]; out [rows][h].
+ *   y [slots][h] of `type`, y_stride between rows; slot, val [rows][k], k <= 2^25; out [rows][h].
  */
 int topk_combine_fwd(const void* y, int64_t y_stride, const int32_t* slot, const float* val, int64_t rows, int64_t k,
                      int64_t slots, int64_t h, int type, void* out, void* stream);

@@ -1,6 +1,7 @@
 // C ABI of the operators behind a router: argument validation and dispatch.  See include/sparse_topk.h.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "../../include/sparse_topk.h"
@@ -9,6 +10,13 @@
 namespace {
 
 constexpr int64_t kMost = int64_t(1) << 31;
+constexpr int64_t kRowsOfLaunch = int64_t(1) << 25;      // routing: up to 64 threads each
+constexpr int64_t kTokensOfLaunch = int64_t(1) << 23;    // weighted sums: up to 256
+constexpr int64_t kPairsOfLaunch = int64_t(1) << 25;     // and their gradients: up to 64
+
+int64_t size_of(int type) { return type == TOPK_TYPE_F32 ? 4 : 2; }
+const void* ahead(const void* p, int64_t bytes) { return p == nullptr ? nullptr : static_cast<const char*>(p) + bytes; }
+void* ahead(void* p, int64_t bytes) { return p == nullptr ? nullptr : static_cast<char*>(p) + bytes; }
 
 bool known_type(int type) { return type >= TOPK_TYPE_F32 && type <= TOPK_TYPE_F16; }
 bool known_score(int score) { return score == TOPK_SCORE_SOFTMAX || score == TOPK_SCORE_SIGMOID; }
@@ -24,7 +32,7 @@ hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
 int check_route(int type, int64_t stride, int64_t rows, int64_t n, int64_t k, int score, double scale) {
   if (rows < 0 || rows >= kMost || n < 1 || n > TOPK_EXPERTS_MAX || k < 1 || k > n || k > TOPK_CHOICES_MAX || stride < 0)
     return TOPK_ERR_INVALID;
-  if (!known_type(type) || !known_score(score) || !std::isfinite(scale)) return TOPK_ERR_INVALID;
+  if (!known_type(type) || !known_score(score) || !std::isfinite(float(scale))) return TOPK_ERR_INVALID;
   return TOPK_OK;
 }
 
@@ -39,7 +47,7 @@ int check_product(const topk::ProductArgs& p, int type) {
 }
 
 int check_combine(const topk::CombineArgs& c, int type) {
-  if (!known_type(type) || c.rows < 0 || c.rows >= kMost || c.k < 1 || c.k >= kMost || c.slots < 0 || c.slots >= kMost ||
+  if (!known_type(type) || c.rows < 0 || c.rows >= kMost || c.k < 1 || c.k > kPairsOfLaunch || c.slots < 0 || c.slots >= kMost ||
       c.h < 1 || c.h >= kMost || c.y_stride < 0 || c.t_stride < 0)
     return TOPK_ERR_INVALID;
   return TOPK_OK;
@@ -60,9 +68,14 @@ int topk_route_fwd(const void* logits, int type, int64_t stride, const float* bi
   if (rows == 0) return TOPK_OK;
   if (logits == nullptr || idx_out == nullptr || val_out == nullptr) return TOPK_ERR_NULL;
   begin();
-  const topk::RouteArgs a{logits, stride, bias, rows, int(n), int(k), int(groups), int(keep_groups), group_top, score,
-                          renormalise != 0, float(scale), idx_out, val_out};
-  return finish(topk::launch_route_fwd(type, a, as_stream(stream)));
+  int launched = 0;
+  for (int64_t r = 0; r < rows && launched == 0; r += kRowsOfLaunch) {
+    const topk::RouteArgs a{ahead(logits, r * stride * size_of(type)), stride, bias, std::min(rows - r, kRowsOfLaunch), int(n),
+                            int(k), int(groups), int(keep_groups), group_top, score, renormalise != 0, float(scale),
+                            idx_out + r * k, val_out + r * k};
+    launched = topk::launch_route_fwd(type, a, as_stream(stream));
+  }
+  return finish(launched);
 }
 
 int topk_route_vjp(const void* logits, int type, int64_t stride, const int32_t* idx, const float* cotangent, int64_t rows,
@@ -72,9 +85,14 @@ int topk_route_vjp(const void* logits, int type, int64_t stride, const int32_t* 
   if (rows == 0) return TOPK_OK;
   if (logits == nullptr || idx == nullptr || cotangent == nullptr || grad_out == nullptr) return TOPK_ERR_NULL;
   begin();
-  const topk::RouteVjpArgs a{logits, stride, idx, cotangent, rows, int(n), int(k), score, renormalise != 0, float(scale),
-                             grad_out};
-  return finish(topk::launch_route_vjp(type, a, as_stream(stream)));
+  int launched = 0;
+  for (int64_t r = 0; r < rows && launched == 0; r += kRowsOfLaunch) {
+    const topk::RouteVjpArgs a{ahead(logits, r * stride * size_of(type)), stride, idx + r * k, cotangent + r * k,
+                               std::min(rows - r, kRowsOfLaunch), int(n), int(k), score, renormalise != 0, float(scale),
+                               ahead(grad_out, r * n * size_of(type))};
+    launched = topk::launch_route_vjp(type, a, as_stream(stream));
+  }
+  return finish(launched);
 }
 
 size_t topk_expert_map_bytes(int64_t rows, int64_t k, int64_t n) {
@@ -142,7 +160,16 @@ int topk_combine_fwd(const void* y, int64_t y_stride, const int32_t* slot, const
   if (rows == 0) return TOPK_OK;
   if ((y == nullptr && slots > 0) || slot == nullptr || out == nullptr) return TOPK_ERR_NULL;
   begin();
-  return finish(topk::launch_combine_fwd(type, c, as_stream(stream)));
+  int launched = 0;
+  for (int64_t t = 0; t < rows && launched == 0; t += kTokensOfLaunch) {
+    topk::CombineArgs part = c;
+    part.rows = std::min(rows - t, kTokensOfLaunch);
+    part.slot = slot + t * k;
+    part.val = val == nullptr ? nullptr : val + t * k;
+    part.out = ahead(out, t * h * size_of(type));
+    launched = topk::launch_combine_fwd(type, part, as_stream(stream));
+  }
+  return finish(launched);
 }
 
 int topk_combine_vjp(const void* y, int64_t y_stride, const int32_t* slot, const float* val, const void* cotangent,
@@ -156,7 +183,18 @@ int topk_combine_vjp(const void* y, int64_t y_stride, const int32_t* slot, const
     return TOPK_ERR_NULL;
   if (val != nullptr && dval_out == nullptr) return TOPK_ERR_NULL;
   begin();
-  return finish(topk::launch_combine_vjp(type, c, as_stream(stream)));
+  const int64_t tokens = kPairsOfLaunch / k;
+  int launched = 0;
+  for (int64_t t = 0; t < rows && launched == 0; t += tokens) {
+    topk::CombineArgs part = c;
+    part.rows = std::min(rows - t, tokens);
+    part.slot = slot + t * k;
+    part.val = val == nullptr ? nullptr : val + t * k;
+    part.t = ahead(cotangent, t * cotangent_stride * size_of(type));
+    part.dval = dval_out == nullptr ? nullptr : dval_out + t * k;
+    launched = topk::launch_combine_vjp(type, part, as_stream(stream));
+  }
+  return finish(launched);
 }
 
 }  // extern "C"

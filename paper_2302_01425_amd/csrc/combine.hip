@@ -143,7 +143,7 @@ int fwd_type(const CombineArgs& a, hipStream_t stream) {
   const int shift = lanes_shift(a.h, sizeof(T), 8);
   const int64_t blocks = ((a.rows << shift) + kThreads - 1) / kThreads;
   const int64_t slices = (a.h * int64_t(sizeof(T)) + (16 << shift) - 1) / (16 << shift);
-  if (blocks >= (int64_t(1) << 31) || slices > 65535) return -1;
+  if (!launchable(blocks * slices, kThreads) || slices > 65535) return -1;
   const dim3 grid = dim3(unsigned(blocks), unsigned(slices)), block(kThreads);
   if (a.h * int64_t(sizeof(T)) < 16) hipLaunchKernelGGL((combine_fwd_kernel<T, true>), grid, block, 0, stream, a, shift);
   else hipLaunchKernelGGL((combine_fwd_kernel<T, false>), grid, block, 0, stream, a, shift);
@@ -153,7 +153,7 @@ template <class T>
 int vjp_type(const CombineArgs& a, hipStream_t stream) {
   const int shift = lanes_shift(a.h, sizeof(T), 6);
   const int64_t blocks = (((a.rows * a.k) << shift) + kThreads - 1) / kThreads;
-  if (blocks >= (int64_t(1) << 31)) return -1;
+  if (!launchable(blocks, kThreads)) return -1;
   const dim3 grid = dim3(unsigned(blocks)), block(kThreads);
   if (a.h * int64_t(sizeof(T)) < 16) hipLaunchKernelGGL((combine_vjp_kernel<T, true>), grid, block, 0, stream, a, shift);
   else hipLaunchKernelGGL((combine_vjp_kernel<T, false>), grid, block, 0, stream, a, shift);

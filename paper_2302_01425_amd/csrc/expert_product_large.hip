@@ -124,7 +124,7 @@ int rows_type(const RowsArgs& g, bool k_contiguous, unsigned blocks, hipStream_t
 int launch_rows_large(int type, RowsArgs g, bool k_contiguous, hipStream_t stream) {
   g.col_tiles = (g.cols + kCols - 1) / kCols;
   const int64_t blocks = rows_blocks(g, kRows);
-  if (blocks >= (int64_t(1) << 31)) return -1;
+  if (!launchable(blocks, kThreads)) return -1;
   if (type == kBF16) return rows_type<bf16>(g, k_contiguous, unsigned(blocks), stream);
   if (type == kF16) return rows_type<f16>(g, k_contiguous, unsigned(blocks), stream);
   return -1;

@@ -207,7 +207,7 @@ template <class TILE, bool TINY>
 int rows_tile(RowsArgs g, bool k_contiguous, hipStream_t stream) {
   g.col_tiles = (g.cols + TILE::kCols - 1) / TILE::kCols;
   const int64_t blocks = rows_blocks(g, TILE::kRows);
-  if (blocks >= (int64_t(1) << 31)) return -1;
+  if (!launchable(blocks, kThreads)) return -1;
   const dim3 grid = dim3(unsigned(blocks)), block(kThreads);
   if (k_contiguous) hipLaunchKernelGGL((rows_tiles_kernel<TILE, true, TINY>), grid, block, 0, stream, g);
   else hipLaunchKernelGGL((rows_tiles_kernel<TILE, false, TINY>), grid, block, 0, stream, g);
@@ -217,7 +217,7 @@ int rows_tile(RowsArgs g, bool k_contiguous, hipStream_t stream) {
 template <class TILE, Load LOAD>
 int weight_tile(WeightArgs g, hipStream_t stream) {
   const int64_t blocks = split_tiles(&g, TILE::kRows, TILE::kCols);
-  if (blocks >= (int64_t(1) << 31)) return -1;
+  if (!launchable(blocks, kThreads)) return -1;
   const dim3 grid = dim3(unsigned(blocks)), block(kThreads);
   if (g.a_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 1, LOAD>), grid, block, 0, stream, g);
   else if (g.b_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 2, LOAD>), grid, block, 0, stream, g);

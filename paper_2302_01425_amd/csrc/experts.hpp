@@ -17,6 +17,9 @@ using f16 = _Float16;
 constexpr int kExpertsMax = 1024;      // experts of a router: a row of scores fits one wavefront
 constexpr int kChoicesMax = 64;        // choices per token
 
+// A launch has fewer than 2^32 threads.
+inline bool launchable(int64_t blocks, int threads) { return blocks < (int64_t(1) << 32) / threads; }
+
 struct RouteArgs {
   const void* logits;
   int64_t stride;            // elements between rows

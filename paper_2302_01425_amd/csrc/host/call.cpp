@@ -6,10 +6,10 @@
 // case (another type, layout or device, overlapping arrays, an explicit stream, a workspace to be made, a mode that
 // watches tensor calls): the Python code then makes the call itself, with its own checks and errors.  Errors of the library
 // are raised from here, by the same function.
-// The operators behind a router take the same way (routing one token 9.8 -> 5.6 us a call, the map of 128 pairs 14.0 -> 7.2).
 //   64 x 16 JVP into given arrays 8.3 -> 4.3 us a call, 16384 x 64 VJP 8.3 -> 6.0 (5.2 on the GPU), compact
 //   output 10.3 -> 6.4, the last two within a tenth from run to run.  What is left of 4.3: 2.7 the launch, 0.7 the Python
 //   function, the rest the checks and the stream.
+// The operators behind a router take the same way: routing one token 9.8 -> 5.6 us a call, the map of 128 pairs 14.0 -> 7.2.
 #include <Python.h>
 
 #include <ATen/ATen.h>

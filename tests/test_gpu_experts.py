@@ -678,3 +678,45 @@ def test_route_of_scores_that_cross_in_float32(gpu, n, k, run):
         ties = np.round(l * 4) / 4
         idx, _ = gpu.topk_route_fwd(put(ties), k, int(sigmoid), bias=put(np.zeros(n)))
         assert np.array_equal(host(idx), ref.route(ties, k, sigmoid, np.zeros(n))[0]), "ties"
+
+
+def test_calls_of_more_rows_than_a_launch_takes(gpu):
+    """Rows at both ends of a call that is cut into several launches."""
+    import torch
+    rows = (1 << 25) + 3
+    at = torch.tensor([0, 1, (1 << 23) - 1, 1 << 23, (1 << 25) - 1, 1 << 25, rows - 1], device="cuda")
+    l = torch.randn((rows, 2), device="cuda").half()
+    idx, val = gpu.topk_route_fwd(l, 1, renormalise=False)
+    want_idx, want_val = gpu.topk_route_fwd(l[at], 1, renormalise=False)
+    assert torch.equal(idx[at], want_idx) and torch.equal(val[at], want_val)
+    assert torch.equal(idx[:, 0], (l[:, 1] > l[:, 0]).int())
+    t = torch.randn((rows, 1), device="cuda")
+    grad = gpu.topk_route_vjp(l, idx, t, renormalise=False)
+    assert torch.equal(grad[at], gpu.topk_route_vjp(l[at], idx[at], t[at].contiguous(), renormalise=False))
+    # the two cancel: an output's rounding each, and float32 roundings of terms up to |t|
+    assert (grad.float().sum(dim=1).abs() <= 2.0 ** -11 * grad.float().abs().sum(dim=1) + 2.0 ** -21 * t.abs()[:, 0] + 2.0 ** -24).all()
+    slot = torch.arange(rows - 1, -1, -1, device="cuda", dtype=torch.int32)[:, None].contiguous()
+    out = gpu.topk_combine_fwd(l, slot, t)
+    # one product, rounded to float32 and to float16, or (a multiplication that ends in float16) to float16 alone
+    def product(got, a):
+        exact = a.double() * t.double()
+        assert ((got.double() - exact).abs() <= (2.0 ** -11 + 2.0 ** -23) * exact.abs() + 2.0 ** -25).all()
+    product(out, l.flip(0))
+    dy, dval = gpu.topk_combine_vjp(l, slot, t, out)
+    product(dy.flip(0), out)
+    want = (out.double() * l.flip(0).double()).sum(dim=1, keepdim=True)
+    # two products, exact in float32, and their sum
+    assert ((dval.double() - want).abs() <= 2.0 ** -23 * (out.double() * l.flip(0).double()).abs().sum(dim=1, keepdim=True)).all()
+
+
+def test_refusals_of_scales_and_counts(gpu):
+    import ctypes
+    import torch
+    l = torch.randn((4, 8), device="cuda")
+    with pytest.raises(gpu.TopkError):
+        gpu.topk_route_fwd(l, 2, scale=1e300)               # infinite in float32
+    with pytest.raises(gpu.TopkError):
+        gpu.topk_route_vjp(l, torch.zeros((4, 1), dtype=torch.int32, device="cuda"), l[:, :1].contiguous(), scale=-1e39)
+    lib, one = gpu.load(), ctypes.c_void_p(256)             # (never read: the counts are refused first)
+    assert lib.topk_combine_fwd(one, 4, one, None, 3, (1 << 25) + 1, 5, 4, 0, one, None) == -1
+    assert lib.topk_combine_vjp(one, 4, one, one, one, 4, (1 << 31) - 1, (1 << 31) - 1, 5, 4, 0, one, one, None) == -1
