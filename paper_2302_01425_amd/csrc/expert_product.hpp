@@ -180,18 +180,19 @@ inline int64_t split_tiles(WeightArgs* g, int64_t rows, int64_t cols) {
   return g->n * share * kDies;
 }
 // Expert and tile of workgroup b, false where there is none.
-__device__ __forceinline__ bool find_weight_tile(const WeightArgs& g, int64_t b, int* expert, int64_t* m, int64_t* col) {
-  const int64_t die = b % kDies, i = b / kDies;
+__device__ __forceinline__ bool find_weight_tile(const WeightArgs& g, uint32_t b, int* expert, int64_t* m, int64_t* col) {
+  const uint32_t die = b % kDies, i = b / kDies, cols = uint32_t(g.col_tiles), die_m = uint32_t(g.die_m);
   if (g.die_cols == 0) {
-    const int64_t tile = die * g.die_m + i % g.die_m;
-    *expert = int(i / g.die_m);
-    *m = tile / g.col_tiles;
-    *col = tile % g.col_tiles;
+    const uint32_t e = i / die_m, tile = die * die_m + i - e * die_m;
+    *expert = int(e);
+    *m = tile / cols;
+    *col = tile % cols;
   } else {
-    const int64_t share = g.die_m * g.die_cols, across = (g.col_tiles + g.die_cols - 1) / g.die_cols, at = i % share;
-    *expert = int(i / share);
-    *m = die / across * g.die_m + at / g.die_cols;
-    *col = die % across * g.die_cols + at % g.die_cols;
+    const uint32_t die_cols = uint32_t(g.die_cols), share = die_m * die_cols, across = (cols + die_cols - 1) / die_cols;
+    const uint32_t e = i / share, at = i - e * share;
+    *expert = int(e);
+    *m = die / across * die_m + at / die_cols;
+    *col = die % across * die_cols + at % die_cols;
   }
   return *m < g.m_tiles && *col < g.col_tiles;
 }
