@@ -277,10 +277,12 @@ struct Here {
   int entry, device;
   void* stream;
 };
-bool here(PyObject* entry, PyObject* stream, Here* h) {
+bool here(PyObject* entry, PyObject* first, PyObject* stream, Here* h) {
   int64_t e;
   if (stream != Py_None || !integer(entry, &e) || e < 0 || e >= kMaxEntries || g_entry[e] == nullptr || !plain_mode())
     return false;
+  // (a tensor of the host is refused by the Python code, also where there is no GPU to ask)
+  if (!THPVariable_CheckExact(first) || !THPVariable_Unpack(first).defined() || !THPVariable_Unpack(first).is_cuda()) return false;
   h->entry = int(e);
   return current_stream(&h->stream, &h->device);
 }
@@ -336,7 +338,7 @@ PyObject* route_fwd(PyObject*, PyObject* const* a, Py_ssize_t count) {
   int64_t k, score, groups, keep, top;
   bool renorm;
   double scale;
-  if (count != 11 || !here(a[0], a[10], &h) || !integer(a[2], &k) || !integer(a[3], &score) || !integer(a[5], &groups) ||
+  if (count != 11 || !here(a[0], a[1], a[10], &h) || !integer(a[2], &k) || !integer(a[3], &score) || !integer(a[5], &groups) ||
       !integer(a[6], &keep) || !integer(a[7], &top) || !flag(a[8], &renorm) || !number(a[9], &scale) || k < 0 || k > 64 ||
       score < 0 || score > 1 || top < 1 || top > 2)
     TOPK_NONE;
@@ -368,7 +370,7 @@ PyObject* route_vjp(PyObject*, PyObject* const* a, Py_ssize_t count) {
   int64_t score;
   bool renorm;
   double scale;
-  if (count != 8 || !here(a[0], a[7], &h) || !integer(a[4], &score) || !flag(a[5], &renorm) || !number(a[6], &scale) ||
+  if (count != 8 || !here(a[0], a[1], a[7], &h) || !integer(a[4], &score) || !flag(a[5], &renorm) || !number(a[6], &scale) ||
       score < 0 || score > 1)
     TOPK_NONE;
   const at::Tensor *x = rows_of(a[1], h.device), *idx = words_matrix(a[2], h.device);
@@ -396,7 +398,7 @@ PyObject* expert_map(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
   Here h;
   int64_t bytes_entry, n, capacity;
-  if (count != 6 || !here(a[0], a[5], &h) || !integer(a[1], &bytes_entry) || bytes_entry < 0 || bytes_entry >= kMaxEntries ||
+  if (count != 6 || !here(a[0], a[2], a[5], &h) || !integer(a[1], &bytes_entry) || bytes_entry < 0 || bytes_entry >= kMaxEntries ||
       g_entry[bytes_entry] == nullptr || !integer(a[3], &n) || !integer(a[4], &capacity) || n < 1 || n > 1024)
     TOPK_NONE;
   const at::Tensor* idx = words_matrix(a[2], h.device);
@@ -451,7 +453,7 @@ PyObject* product_fwd(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
   Here h;
   Product p;
-  if (count != 7 || !here(a[0], a[6], &h) || !product_args(a + 1, h.device, &p)) TOPK_NONE;
+  if (count != 7 || !here(a[0], a[1], a[6], &h) || !product_args(a + 1, h.device, &p)) TOPK_NONE;
   at::Tensor out = at::empty({p.slots, p.ho}, at::TensorOptions().dtype(p.x->scalar_type()).device(p.x->device()));
   const void *xp = data(p.x), *wp = data(p.w), *fp = data(p.offset), *sp = data(p.source);
   const int64_t stride = p.x->stride(0), m = p.x->size(0);
@@ -473,7 +475,7 @@ PyObject* product_vjp(PyObject*, PyObject* const* a, Py_ssize_t count) {
   Here h;
   Product p;
   bool want_x, want_w;
-  if (count != 10 || !here(a[0], a[9], &h) || !product_args(a + 1, h.device, &p) || !flag(a[7], &want_x) || !flag(a[8], &want_w) ||
+  if (count != 10 || !here(a[0], a[1], a[9], &h) || !product_args(a + 1, h.device, &p) || !flag(a[7], &want_x) || !flag(a[8], &want_w) ||
       !(want_x || want_w))
     TOPK_NONE;
   const at::Tensor* t = rows_of(a[6], h.device);
@@ -515,7 +517,7 @@ PyObject* combine_fwd(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
   Here h;
   Combine c;
-  if (count != 5 || !here(a[0], a[4], &h) || !combine_args(a + 1, h.device, &c)) TOPK_NONE;
+  if (count != 5 || !here(a[0], a[1], a[4], &h) || !combine_args(a + 1, h.device, &c)) TOPK_NONE;
   at::Tensor out = at::empty({c.rows, c.width}, at::TensorOptions().dtype(c.y->scalar_type()).device(c.y->device()));
   const void *yp = data(c.y), *sp = data(c.slot), *vp = data(c.val);
   const int64_t stride = c.y->stride(0);
@@ -535,7 +537,7 @@ PyObject* combine_vjp(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
   Here h;
   Combine c;
-  if (count != 7 || !here(a[0], a[6], &h) || !combine_args(a + 1, h.device, &c)) TOPK_NONE;
+  if (count != 7 || !here(a[0], a[1], a[6], &h) || !combine_args(a + 1, h.device, &c)) TOPK_NONE;
   const at::Tensor* t = rows_of(a[4], h.device);
   if (t == nullptr || t->scalar_type() != c.y->scalar_type() || t->size(0) != c.rows || t->size(1) != c.width) TOPK_NONE;
   const auto values = at::TensorOptions().dtype(c.y->scalar_type()).device(c.y->device());
