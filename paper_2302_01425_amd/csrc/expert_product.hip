@@ -27,16 +27,23 @@ int64_t row_tiles(const RowsArgs& g, int64_t rows, int64_t cols) {
 }
 
 // Which kernel takes the rows (bfloat16, us):
+//   few rows, 64 x 64 / four rows at a time (each W on its first call; 1, 4, 16 tokens x 2 to 8 experts, 1 to 16 tokens x 4 to 64):
+//     4096 -> 1024 38 / 9, 47 / 15, 47 / 25 (64 tokens: 47 / 41 with 8 places each), 2048 -> 4096 22 / 11, 30 / 32 (512 tiles), 2048 ->
+//     1024 21 / 9, 27 / 19, 32 / 33 (8 tokens, 512 tiles); float32 112 / 11, 129 / 22, 130 / 34; 68 / 16, 96 / 43, 97 / 65; 59 / 11,
+//     69 / 27, 131 / 71 (64 tokens, 4 places each, 210 / 126): there the matrix instructions of 32 rows take longer than the loads.
 //   float32, 64 x 64 / 128 x 128: 16 experts of 64, 512 rows, 1024 -> 1024 49 / 88, 184 / 225; 4 of 4096, 1024 -> 2048 646 / 640.
 //   whole parts, 64 x 64 / 256 x 256: 2048 -> 4096, 16 experts of 8, 64, 128, 256 rows on average 37 / 41, 60 / 68, 99 / 78,
 //     170 / 116; 8 experts of 128 rows, 1024 -> 1024, 32 tiles of 256 x 256: 16 / 34; 16 of 250, 1000 -> 2008, 128 tiles 55 / 40.
 //   others, 64 x 64 / 128 x 128: 64 experts of 32, 64, 256 rows, 1025 -> 2047 68 / 80, 109 / 113, 284 / 215; 16 of 250, 1001 ->
 //     2005 62 / 58; 10 of 300, 515 -> 1001 (240 tiles) 20 / 18, 1001 -> 515 (150 tiles) 18 / 25; 8 of 2048, 2001 -> 3001 586 / 388.
 int launch_rows(int type, const RowsArgs& g, bool k_contiguous, hipStream_t stream) {
-  if (type == kF32) return launch_rows_tiles(type, g, k_contiguous, kSmall, stream);
   const int64_t share = even_share(g.slots, g.n);
   const int s = size_of(type);
   // (limit 0: there is no row that could be read in the place of one that is out of range)
+  const bool few = (share <= 8 && cut(share, 4) * row_tiles(g, 64, 64) < 512) || (type == kF32 && share <= 4);
+  if (few && g.limit > 0 && g.depth * s >= 16 && (k_contiguous || g.cols >= 32))
+    return launch_rows_few(type, g, k_contiguous, stream);
+  if (type == kF32) return launch_rows_tiles(type, g, k_contiguous, kSmall, stream);
   const bool whole = g.limit > 0 && whole_parts(g.a, g.a_stride, g.depth, s) &&
                      whole_parts(g.w, g.w_stride, k_contiguous ? g.depth : g.cols, s) && g.w_expert * s % 16 == 0;
   if (whole && share >= 96 && row_tiles(g, 256, 256) >= 96) return launch_rows_large(type, g, k_contiguous, stream);

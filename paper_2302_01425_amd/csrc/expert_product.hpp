@@ -201,6 +201,8 @@ inline int64_t rows_blocks(const RowsArgs& g, int size) {
   return (g.slots / size + min(int64_t(g.n), g.slots)) * g.col_tiles + kDies * kRunMost;
 }
 
+// few rows per expert, limit > 0; W contiguous in n: of 32 columns at least
+int launch_rows_few(int type, const RowsArgs& g, bool k_contiguous, hipStream_t stream);
 int launch_rows_large(int type, RowsArgs g, bool k_contiguous, hipStream_t stream);
 // tiles of expert_product_tiles.hip; kWideDirect: dW of whole, aligned parts only.  float32 takes kSmall
 enum TileKind { kSmall, kMiddle, kWideDirect };

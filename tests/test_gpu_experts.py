@@ -720,3 +720,42 @@ def test_refusals_of_scales_and_counts(gpu):
     lib, one = gpu.load(), ctypes.c_void_p(256)             # (never read: the counts are refused first)
     assert lib.topk_combine_fwd(one, 4, one, None, 3, (1 << 25) + 1, 5, 4, 0, one, None) == -1
     assert lib.topk_combine_vjp(one, 4, one, one, one, 4, (1 << 31) - 1, (1 << 31) - 1, 5, 4, 0, one, one, None) == -1
+
+
+# few places per expert, as in decoding: any length of k and number of columns, one expert with all tokens
+@pytest.mark.parametrize("rows,k,n,h,ho", [(1, 1, 1, 4, 32), (1, 2, 8, 4097, 1640), (4, 2, 8, 1003, 2049), (3, 1, 64, 520, 36), (2, 8, 16, 8, 3001),
+                                           (8, 1, 8, 2000, 33), (16, 1, 4, 515, 259), (5, 3, 6, 4, 700), (1, 1, 3, 2051, 31), (7, 2, 1024, 64, 64)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("one", [False, True])
+def test_products_of_few_places(gpu, rows, k, n, h, ho, dtype, one):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(rows + h)
+    dt = getattr(torch, dtype)
+    idx = torch.rand((rows, n), generator=g, device="cuda").argsort(dim=1)[:, :k].to(torch.int32).contiguous()
+    if one:
+        idx[:, 0] = n - 1                                       # (every token, and no other: the rest are empty places)
+        idx[:, 1:] = -1
+    _, source, offset, _ = gpu.topk_expert_map(idx, n)
+    x = torch.randn((rows + 2, h), generator=g, device="cuda").to(dt)
+    x[rows:] = float("nan")                                     # (rows that no place names)
+    t = torch.randn((rows * k, ho), generator=g, device="cuda").to(dt)
+    w = torch.randn((n, ho, h), generator=g, device="cuda").to(dt)
+    at = offset.tolist()
+    t[at[n]:] = float("inf")
+    for transposed in (False, True):
+        for shift in (0, 1):
+            wd = w.transpose(1, 2).contiguous().transpose(1, 2) if transposed else w
+            xd = strided(host(x), dtype, 3, 1) if shift else x
+            out = torch.full((rows * k, ho), MARK, device="cuda", dtype=dt)
+            gpu.topk_expert_product_fwd(xd, wd, offset, source=source, k=k, out=out)
+            dx = torch.full((rows * k, h), MARK, device="cuda", dtype=dt)
+            gpu.topk_expert_product_vjp(xd, wd, offset, t, source=source, k=k, dx_out=dx, want_w=False)
+            assert (out[at[n]:] == MARK).all() and (dx[at[n]:] == MARK).all()
+            for e in range(n):
+                if at[e] == at[e + 1]:
+                    continue
+                part = slice(at[e], at[e + 1])
+                xe, te, we = x[(source[part] // k).long()].double(), t[part].double(), w[e].double()
+                for have, a, b, terms, name in ((out[part], xe, we.t().contiguous(), h, "out"), (dx[part], te, we, ho, "dx")):
+                    want, size = host(a @ b), host(a.abs() @ b.abs())
+                    within(host(have), want, (terms + 2) * 2 * U * size + HALF[dtype] * np.abs(want) + TINY[dtype], (name, e))
