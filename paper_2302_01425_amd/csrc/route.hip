@@ -8,7 +8,7 @@
 //
 // A row lies in the registers of 8 to 64 lanes and is read once; k rounds take the largest each.  Bound by the launch below some
 // 1000 rows (5 us a call), by instructions above: a round of 32 lanes x 8 elements is 87 of them.  16384 x 64 float32, softmax, k = 2:
-// 4.2 us, 1.0 TB/s; 8192 x 256 bfloat16, sigmoid, bias, 8 groups, k = 8: 13 us a call, 0.35 TB/s (16 lanes x 16 elements: 12 to
+// 4.2 us, 1.0 TB/s; 8192 x 256 bfloat16, sigmoid, bias, 8 groups, k = 8: 12.5 us a call, 0.38 TB/s (16 lanes x 16 elements: 12 to
 // 17 us, and 2 us more for few rows).
 #include <cmath>
 
