@@ -223,10 +223,15 @@ __device__ __forceinline__ int choose(const RouteArgs& a, const Lane<E>& w, bool
       rank += other > score || (other == score && o < w.g);
     }
     if (sizeof(KEY) == 4 && scored) {
-      const float in = rank < a.keep ? float(score) : INFINITY, out = rank < a.keep || w.g >= a.groups ? kNone : float(score);
+      // A group's score is off by its scores' errors and by two roundings of each of the c it is the sum of, which may be far
+      // larger than their sum (biases of both signs).  The groups are sure if no score that stays comes down to one that goes
+      // when both move by that (twice the roundings leave room for those of this sum), and if float32 held all of them.
+      const bool any = first > KEY(-INFINITY);
+      const float size = any ? fabsf(float(first)) + (a.top == 2 && second > KEY(-INFINITY) ? fabsf(float(second)) : 0.0f) : 0.0f;
+      const float off = 2.0f * (rel + err) + 0x1p-22f * (1.0f + size);
+      const float in = rank < a.keep ? float(score) - off : INFINITY, out = rank < a.keep || w.g >= a.groups ? kNone : float(score) + off;
       const float low = -group_max<GL>(-in), high = group_max<GL>(out);
-      // (two scores of a softmax add up to 1 at most, two others to 2)
-      good = high == kNone || low - high > 2.0f * (2.0f * (rel + err) + 0x1p-23f * (1.0f + fabsf(low) + fabsf(high)));
+      good = (high == kNone || low > high) && size < 0x1p126f;
     }
     if (rank >= a.keep) {
 #pragma unroll

@@ -1,0 +1,58 @@
+"""The operators behind a router (tests/test_gpu_experts.py) where a call's values or sizes are unusual: scores of groups that
+float32 cannot tell apart, infinities and NaN at places that are not there, calls that take more than one launch."""
+import numpy as np
+import pytest
+
+from tests import experts_reference as ref
+from tests.test_gpu_experts import gpu, host, put  # noqa: F401  (gpu: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- route: scores of groups ----------------------------------------------------------------------------------------------
+
+# Groups whose scores differ by a few roundings of what they are made of: `size` the biases of the two largest, +size and -size
+# (top 2: their sum is small, its roundings are not) or +size in every group (top 1).
+@pytest.mark.parametrize("n,groups,keep", [(4, 2, 1), (60, 6, 2), (64, 8, 3), (1024, 32, 5)])
+@pytest.mark.parametrize("size", [0.5, 10.0, 1e3, 1e5])
+@pytest.mark.parametrize("top", [1, 2])
+def test_route_of_groups_that_cross_in_float32(gpu, n, groups, keep, size, top):
+    rows, width = 200, n // groups
+    r = np.random.default_rng(n + top)
+    for sigmoid in (False, True):
+        bias = np.full((groups, width), -3.0 * size, np.float32)
+        bias[:, 0] = size * (1.0 + 0.5 * r.random(groups)) if top == 2 else size
+        bias[:, 1] = -bias[:, 0] if top == 2 else 0.0
+        if top == 2:
+            bias[1::2, :2] = 0.0
+        bias = bias.reshape(-1)
+        l = r.normal(size=(rows, groups, width)).astype(np.float32)
+        l[:, 1:, :2] = l[:, :1, :2]
+        l[:, 1:, 0] += (2.0 ** -12 * r.normal(size=(rows, groups - 1)) * r.choice([1.0, 0.1, 0.01], size=(rows, 1))).astype(np.float32)
+        l = l.reshape(rows, n)
+        # rows whose decision is within the roundings of float64 decide nothing here
+        c = ref.scores(l, sigmoid) + bias.astype(np.float64)
+        score = np.sort(-np.sort(-c.reshape(rows, groups, width), axis=2)[:, :, :top].sum(axis=2), axis=1)[:, ::-1]
+        clear = score[:, keep - 1] - score[:, keep] > 32 * 2.0 ** -53 * (1.0 + 2.0 * size)
+        assert clear.sum() > rows // 2
+        k = min(2, keep * width)
+        want = ref.route(l, k, sigmoid, bias, groups, keep, top)[0]
+        print("case", n, groups, keep, size, top, sigmoid, int(clear.sum()), flush=True)
+        got = host(gpu.topk_route_fwd(put(l), k, int(sigmoid), bias=put(bias), groups=groups, keep_groups=keep, group_top=top)[0])
+        bad = clear & (got != want).any(axis=1)
+        assert not bad.any(), (int(bad.sum()), np.flatnonzero(bad)[:4], got[bad][:4], want[bad][:4])
+
+
+def test_route_of_groups_whose_scores_float32_cannot_hold(gpu):
+    """Sums of two biases above the largest float32, infinite ones, and groups that are out."""
+    l = np.zeros((3, 8), np.float32)
+    l[1] = np.arange(8) / 4
+    l[2, 6:] = -np.inf
+    for bias in ([3.0e38, 3.0e38, 3.2e38, 3.2e38, 0, 0, 3.1e38, 3.3e38], [3.0e38, -3.0e38, 1.0, 1.0, 0.5, 0.5, 3.3e38, 3.3e38],
+                 [np.inf, 0, 1, 1, np.inf, 0.5, 3.0e38, 3.0e38], [-np.inf, -np.inf, -3e38, -3e38, -3.1e38, -3.1e38, 0, np.nan]):
+        b = np.array(bias, np.float32)
+        for sigmoid in (False, True):
+            for keep in (1, 2, 3):
+                want = ref.route(l, 2, sigmoid, b, 4, keep, 2)[0]
+                got = host(gpu.topk_route_fwd(put(l), 2, int(sigmoid), bias=put(b), groups=4, keep_groups=keep, group_top=2)[0])
+                assert np.array_equal(got, want), (bias, sigmoid, keep, got, want)
