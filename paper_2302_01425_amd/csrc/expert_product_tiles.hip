@@ -163,8 +163,8 @@ __global__ __launch_bounds__(kThreads, 2) void rows_tiles_kernel(RowsArgs g) {
   typename TILE::Sums acc;
   clear(acc);
   sum_staged<TILE, IA, IB, false>(lds, a, b, Table{}, g.depth, acc);
-  store_tile(acc, f.begin + TILE::wave_row(), f.end, n0 + TILE::wave_col(), g.cols, nullptr, Divisor{}, 0, static_cast<T*>(g.c),
-             g.cols);
+  store_tile(acc, f.begin + TILE::wave_row(), f.end, n0 + TILE::wave_col(), g.cols, g.source, g.div, g.limit,
+             static_cast<T*>(g.c), g.cols);
 }
 
 // LIST: which operand's rows are found through source (0: neither, 1: A, 2: B)

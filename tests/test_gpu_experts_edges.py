@@ -56,3 +56,42 @@ def test_route_of_groups_whose_scores_float32_cannot_hold(gpu):
                 want = ref.route(l, 2, sigmoid, b, 4, keep, 2)[0]
                 got = host(gpu.topk_route_fwd(put(l), 2, int(sigmoid), bias=put(b), groups=4, keep_groups=keep, group_top=2)[0])
                 assert np.array_equal(got, want), (bias, sigmoid, keep, got, want)
+
+
+# ---- products: places whose source is out of range -------------------------------------------------------------------------
+
+def with_holes(rng, places, rows, k):
+    """Sources with some out of the rows, and which."""
+    import torch
+    source = rng.integers(0, max(1, rows * k), size=places).astype(np.int32)
+    gone = rng.random(places) < 0.25
+    gone[0] = True
+    bad = np.array([-1, -2 ** 31, rows * k, 2 ** 31 - 1], np.int32)
+    source[gone] = bad[rng.integers(0, 4, size=int(gone.sum()))]
+    return source, torch.from_numpy(gone).cuda()
+
+
+# n experts of `share` places, h -> ho: few places, 256 x 256, 128 x 128, 64 x 64, rows shorter than 16 bytes, no rows of x at all
+@pytest.mark.parametrize("n,share,rows,h,ho", [(4, 3, 6, 520, 96), (8, 1024, 300, 64, 1024), (8, 512, 300, 67, 899), (3, 50, 20, 72, 136),
+                                               (3, 50, 20, 71, 137), (2, 20, 9, 3, 66), (2, 20, 0, 40, 40)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("transposed", [False, True])
+def test_product_of_absent_rows_is_zero_whatever_w_holds(gpu, n, share, rows, h, ho, dtype, transposed):
+    import torch
+    k = 2
+    source, gone = with_holes(np.random.default_rng(n * h), n * share, rows, k)
+    if rows == 0:
+        gone[:] = True
+    g = torch.Generator(device="cuda").manual_seed(h)
+    dt = getattr(torch, dtype)
+    x = torch.randn((rows, h), generator=g, device="cuda").to(dt)
+    w = torch.randn((n, ho, h), generator=g, device="cuda").to(dt)
+    w[:, 1, h // 2], w[:, ho - 1, 0], w[0, :, h - 1] = float("inf"), float("nan"), -float("inf")
+    w = w.transpose(1, 2).contiguous().transpose(1, 2) if transposed else w
+    offset = torch.arange(0, n * share + 1, share, dtype=torch.int32, device="cuda")
+    out = gpu.topk_expert_product_fwd(x, w, offset, source=put(source, "int32"), k=k)
+    assert (out[gone] == 0).all()
+    if rows:
+        there = torch.where(gone, 0, put(source, "int32")).to(torch.int32)
+        want = gpu.topk_expert_product_fwd(x, w, offset, source=there, k=k)
+        assert torch.equal(out[~gone].nan_to_num(nan=7.0), want[~gone].nan_to_num(nan=7.0))
