@@ -394,7 +394,8 @@ int topk_expert_product_fwd(const void* x, int64_t x_stride, int64_t m, const vo
 /*
  * Its gradients (either output may be NULL):  dx_out[s] = W[e]^T cotangent[s], per PLACE, rows behind offset[n] left as they
  * were (with source, topk_combine_fwd(dx_out, slot, NULL, ..) sums them to the rows of x);
- * dW_out[e] = sum over e's places of cotangent[s] x[r(s)]^T, zeros for an expert without places.
+ * dW_out[e] = sum over e's places of cotangent[s] x[r(s)]^T, places whose source is out of range left out, zeros for an
+ * expert without places.
  *   cotangent [slots][ho]; dx_out [slots][h]; dw_out [n][ho][h] contiguous where w_in is 1, otherwise [n][h][ho].
  */
 int topk_expert_product_vjp(const void* x, int64_t x_stride, int64_t m, const void* w, int64_t w_expert, int64_t w_out,

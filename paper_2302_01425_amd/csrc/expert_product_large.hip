@@ -29,9 +29,9 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& g, const Found& f, cha
   using IB = Image<T, B_KC, kCols, kThreads, kStep>;
   const int64_t n0 = f.col * kCols;
   const T* w = static_cast<const T*>(g.w) + f.expert * g.w_expert;
-  Direct<IA, false> a;
+  Direct<IA, kInOrder> a;
   a.init_rows(g.a, g.a_stride, g.source, g.div, g.limit, f.begin, f.end);
-  Direct<IB, false> b;
+  Direct<IB, kInOrder> b;
   if constexpr (B_KC) b.init_rows(w, g.w_stride, nullptr, Divisor{}, 0, n0, g.cols);
   else b.init_columns(w, g.w_stride, nullptr, n0, g.cols, 0);
 

@@ -71,24 +71,29 @@ __device__ __forceinline__ void sum_direct(char* lds, const LA& a, const LB& b, 
       if ((k0 & (kTable - 1)) == 0) table.fill<kThreads>(k0, depth);
     }
   };
-  const auto issue = [&](int i, int64_t k0, int stage) {   // (steps behind the last are loaded as zeros)
-    if (i < IA::kParts) a.issue_part(i, k0, depth, lds0 + stage * TILE::kStageBytes);
-    else b.issue_part(i - IA::kParts, k0, depth, lds0 + stage * TILE::kStageBytes + IA::kBytes);
+  const auto there = [&](int64_t k0) {
+    if constexpr (LISTED) return table.bits(k0);
+    else return 0u;
+  };
+  const auto issue = [&](int i, int64_t k0, uint32_t bits, int stage) {   // (steps behind the last are loaded as zeros)
+    if (i < IA::kParts) a.issue_part(i, k0, depth, lds0 + stage * TILE::kStageBytes, bits);
+    else b.issue_part(i - IA::kParts, k0, depth, lds0 + stage * TILE::kStageBytes + IA::kBytes, bits);
   };
 #pragma unroll
   for (int stage = 0; stage < 2; ++stage) {
     fill(stage * IA::kStepK);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) issue(i, stage * IA::kStepK, stage);
+    for (int i = 0; i < kLoads; ++i) issue(i, stage * IA::kStepK, there(stage * IA::kStepK), stage);
   }
   int stage = 0;
   for (int64_t k0 = 0; k0 < depth; k0 += IA::kStepK) {
     wait_stage<kLoads>();
     fill(k0 + 2 * IA::kStepK);
+    const uint32_t bits = there(k0 + 2 * IA::kStepK);
     const int other = stage == 0 ? 2 : stage - 1;
     multiply<TILE, IA, IB>(lds + stage * TILE::kStageBytes, acc, [&](int turn, int turns) {
 #pragma unroll
-      for (int i = turn * kLoads / turns; i < (turn + 1) * kLoads / turns; ++i) issue(i, k0 + 2 * IA::kStepK, other);
+      for (int i = turn * kLoads / turns; i < (turn + 1) * kLoads / turns; ++i) issue(i, k0 + 2 * IA::kStepK, bits, other);
       __builtin_amdgcn_sched_barrier(0);
     });
     stage = stage == 2 ? 0 : stage + 1;
@@ -155,9 +160,9 @@ __global__ __launch_bounds__(kThreads, 2) void rows_tiles_kernel(RowsArgs g) {
   using IB = typename TILE::template B<B_KC>;
   const int64_t n0 = tile_start(f.col, TILE::kCols, g.cols);
   const T* w = static_cast<const T*>(g.w) + f.expert * g.w_expert;
-  Staged<IA, false, TINY> a;
+  Staged<IA, kInOrder, TINY> a;
   a.init_rows(g.a, g.a_stride, g.source, g.div, g.limit, f.begin, f.end);
-  Staged<IB, false, TINY> b;
+  Staged<IB, kInOrder, TINY> b;
   if constexpr (B_KC) b.init_rows(w, g.w_stride, nullptr, Divisor{}, 0, n0, g.cols);
   else b.init_columns(w, g.w_stride, nullptr, n0, g.cols, 0);
   typename TILE::Sums acc;
@@ -174,6 +179,7 @@ __global__ __launch_bounds__(kThreads, 2) void weight_tiles_kernel(WeightArgs g)
   using T = typename TILE::T;
   __shared__ __attribute__((aligned(1024))) char lds[(LOAD == kDirect ? 3 : 2) * TILE::kStageBytes];
   __shared__ int32_t rows[LIST != 0 ? kTable : 1];
+  __shared__ uint32_t there[LIST != 0 ? kTable / 32 : 1];
   int e;
   int64_t m0, n0;
   if (!find_weight_tile(g, blockIdx.x, &e, &m0, &n0)) return;
@@ -190,13 +196,15 @@ __global__ __launch_bounds__(kThreads, 2) void weight_tiles_kernel(WeightArgs g)
   n0 = LOAD == kDirect ? n0 * TILE::kCols : tile_start(n0, TILE::kCols, g.cols);
   using IA = typename TILE::template A<false>;
   using IB = typename TILE::template B<false>;
-  std::conditional_t<LOAD == kDirect, Direct<IA, LIST == 1>, Staged<IA, LIST == 1, LOAD == kTiny>> a;
+  constexpr Order kOrderA = LIST == 0 ? kInOrder : LIST == 1 ? kListed : kInOrderWhereListed;
+  constexpr Order kOrderB = LIST == 0 ? kInOrder : LIST == 2 ? kListed : kInOrderWhereListed;
+  std::conditional_t<LOAD == kDirect, Direct<IA, kOrderA>, Staged<IA, kOrderA, LOAD == kTiny>> a;
   a.init_columns(g.a, g.a_stride, rows, m0, g.m, begin);
-  std::conditional_t<LOAD == kDirect, Direct<IB, LIST == 2>, Staged<IB, LIST == 2, LOAD == kTiny>> b;
+  std::conditional_t<LOAD == kDirect, Direct<IB, kOrderB>, Staged<IB, kOrderB, LOAD == kTiny>> b;
   b.init_columns(g.b, g.b_stride, rows, n0, g.cols, begin);
   typename TILE::Sums acc;
   clear(acc);
-  const Table table{rows, LIST == 0 ? nullptr : (LIST == 1 ? g.a_source : g.b_source) + begin, g.div,
+  const Table table{rows, there, LIST == 0 ? nullptr : (LIST == 1 ? g.a_source : g.b_source) + begin, g.div,
                     LIST == 1 ? g.a_limit : g.b_limit};
   if constexpr (LOAD == kDirect) sum_direct<TILE, IA, IB, LIST != 0>(lds, a, b, table, end - begin, acc);
   else sum_staged<TILE, IA, IB, LIST != 0>(lds, a, b, table, end - begin, acc);

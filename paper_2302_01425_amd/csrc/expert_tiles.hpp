@@ -76,6 +76,7 @@ constexpr int kTable = 1024;               // places whose rows are looked up at
 // Rows of x behind an expert's places, kTable places at a time (dW): -1 where there is none.
 struct Table {
   int32_t* rows;             // LDS, kTable of them
+  uint32_t* there;           // LDS, a bit each
   const int32_t* source;     // of the expert's first place
   Divisor div;
   int64_t limit;
@@ -86,10 +87,15 @@ struct Table {
     for (int i = threadIdx.x; i < kTable; i += THREADS) {
       const int pair = k0 + i < depth ? source[k0 + i] : -1;
       const int row = quotient(max(pair, 0), div);
-      rows[i] = pair >= 0 && row < limit ? row : -1;
+      const bool in = pair >= 0 && row < limit;
+      rows[i] = in ? row : -1;
+      const unsigned long long bits = __ballot(in);
+      if ((i & 31) == 0) there[i >> 5] = uint32_t(bits >> (i & 32));
     }
     __syncthreads();
   }
+  // bits of the places k0 (a multiple of 32) ..
+  __device__ __forceinline__ uint32_t bits(int64_t k0) const { return there[(int(k0) & (kTable - 1)) >> 5]; }
 };
 
 // 16 bytes per lane from `from` to LDS at `to` (the same for the wavefront) + 16 * lane.  Not waited for, and unknown to the
@@ -107,13 +113,17 @@ __device__ __forceinline__ uint32_t lds_address(const char* p) {
   return uint32_t(uintptr_t((const __attribute__((address_space(3))) char*)p));
 }
 
-// An operand whose rows are made of whole, aligned parts, loaded to LDS without passing through registers.
-// LISTED (not KC): the row of a k is looked up in `table`.  k counts from the sum's first.
-template <class IMAGE, bool LISTED>
+// Which row of an operand (not KC) belongs to a k: the k-th; the one that `table` lists; the k-th, but zeros where the table lists
+// none (dW: a place without a row of x adds nothing, whatever its cotangent holds; 0 * infinity would be NaN).
+enum Order { kInOrder, kListed, kInOrderWhereListed };
+
+// An operand whose rows are made of whole, aligned parts, loaded to LDS without passing through registers.  k counts from the
+// sum's first.
+template <class IMAGE, Order ORDER>
 struct Direct {
   using T = typename IMAGE::Type;
   static constexpr bool KC = IMAGE::kKC;
-  const char* p[IMAGE::kParts];    // the part at k = 0 (LISTED: its column of row 0)
+  const char* p[IMAGE::kParts];    // the part at k = 0 (kListed: its column of row 0)
   int64_t stride;                  // bytes between rows (not KC)
   const int32_t* table;
 
@@ -137,19 +147,24 @@ struct Direct {
     for (int i = 0; i < IMAGE::kParts; ++i) {
       const int64_t at = min(first + IMAGE::part_of(i) * IMAGE::N, end - IMAGE::N);
       p[i] = static_cast<const char*>(base) + at * int64_t(sizeof(T));
-      if (!LISTED) p[i] += (k_begin + IMAGE::row_of(i)) * stride;
+      if (ORDER != kListed) p[i] += (k_begin + IMAGE::row_of(i)) * stride;
     }
   }
 
-  // part i of the step k0 .. to LDS at `to` (of the step's image), zeros from `depth` on; without branches
-  __device__ __forceinline__ void issue_part(int i, int64_t k0, int64_t depth, uint32_t to) const {
+  // part i of the step k0 .. to LDS at `to` (of the step's image), zeros from `depth` on; without branches.  `there`: the table's
+  // bits of the step, read once (both gradients of 8192 tokens x 2, 32 experts, 2048 -> 4096: 745 us, 748 with a look into the
+  // table for every part, 739 without either; with code of its own for steps that have such a place the sums left the registers)
+  __device__ __forceinline__ void issue_part(int i, int64_t k0, int64_t depth, uint32_t to, uint32_t there = 0) const {
     const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
     const char* zeros = reinterpret_cast<const char*>(&zero_part);
     const char* from;
-    if constexpr (LISTED) {
+    if constexpr (ORDER == kListed) {
       const int row = table[(int(k0) + IMAGE::row_of(i)) & (kTable - 1)];
       // (the row is selected before the product: a product in one of two ways would be a branch)
       from = (row >= 0 ? p[i] : zeros) + uint64_t(uint32_t(max(row, 0))) * uint32_t(stride);
+    } else if constexpr (ORDER == kInOrderWhereListed) {
+      static_assert(IMAGE::kStepK == 32, "a word per step");
+      from = (there >> IMAGE::row_of(i) & 1u) != 0 ? p[i] + k0 * stride : zeros;
     } else {
       from = p[i] + k0 * (KC ? int64_t(sizeof(T)) : stride);
       const int left = int(min(depth - k0, int64_t(IMAGE::kStepK)));
@@ -163,7 +178,7 @@ struct Direct {
 // is one of 16 bytes, and every step has as many, so that the waits count exactly: a part that crosses the end of its row is
 // read from N elements before the end and shifted into place when it is written.  TINY: rows shorter than that, element by
 // element.
-template <class IMAGE, bool LISTED, bool TINY>
+template <class IMAGE, Order ORDER, bool TINY>
 struct Staged {
   using T = typename IMAGE::Type;
   static constexpr bool KC = IMAGE::kKC;
@@ -197,7 +212,7 @@ struct Staged {
     for (int i = 0; i < IMAGE::kParts; ++i) {
       // (columns behind the end are not stored)
       p[i] = static_cast<const T*>(base) + first + (TINY ? IMAGE::part_of(i) * N : min(int64_t(IMAGE::part_of(i) * N), edge - N));
-      if (!LISTED) p[i] += (k_begin + IMAGE::row_of(i)) * stride;
+      if (ORDER != kListed) p[i] += (k_begin + IMAGE::row_of(i)) * stride;
     }
   }
 
@@ -231,12 +246,13 @@ struct Staged {
       if constexpr (KC) {
         there = p[i] != nullptr;
         from = p[i] + k0;
-      } else if constexpr (LISTED) {
+      } else if constexpr (ORDER == kListed) {
         const int row = table[(int(k0) + IMAGE::row_of(i)) & (kTable - 1)];
         there = row >= 0;
         from = p[i] + row * stride;
       } else {
-        there = k0 + IMAGE::row_of(i) < depth;
+        if constexpr (ORDER == kInOrderWhereListed) there = table[(int(k0) + IMAGE::row_of(i)) & (kTable - 1)] >= 0;
+        else there = k0 + IMAGE::row_of(i) < depth;
         from = p[i] + k0 * stride;
       }
       if constexpr (TINY) {

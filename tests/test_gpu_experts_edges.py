@@ -95,3 +95,32 @@ def test_product_of_absent_rows_is_zero_whatever_w_holds(gpu, n, share, rows, h,
         there = torch.where(gone, 0, put(source, "int32")).to(torch.int32)
         want = gpu.topk_expert_product_fwd(x, w, offset, source=there, k=k)
         assert torch.equal(out[~gone].nan_to_num(nan=7.0), want[~gone].nan_to_num(nan=7.0))
+
+
+# n experts of `share` places, h x ho of W: 128 x 256 loaded straight to LDS, 128 x 128, 64 x 64, rows shorter than 16 bytes
+@pytest.mark.parametrize("n,share,rows,h,ho", [(32, 70, 300, 1024, 256), (4, 1100, 300, 2048, 1024), (64, 40, 300, 389, 259), (3, 1100, 300, 72, 136),
+                                               (3, 50, 20, 71, 137), (2, 20, 9, 3, 66), (2, 20, 0, 40, 40)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("transposed", [False, True])
+def test_weight_gradient_leaves_absent_rows_out(gpu, n, share, rows, h, ho, dtype, transposed):
+    """A place whose source is out of range adds nothing to dW, whatever its cotangent holds."""
+    import torch
+    k = 2
+    source, gone = with_holes(np.random.default_rng(n * h), n * share, rows, k)
+    if rows == 0:
+        gone[:] = True
+    g = torch.Generator(device="cuda").manual_seed(h)
+    dt = getattr(torch, dtype)
+    x = torch.randn((rows, h), generator=g, device="cuda").to(dt)
+    w = torch.zeros((n, h, ho), dtype=dt, device="cuda").transpose(1, 2) if transposed else torch.zeros((n, ho, h), dtype=dt, device="cuda")
+    t = torch.randn((n * share, ho), generator=g, device="cuda").to(dt)
+    offset = torch.arange(0, n * share + 1, share, dtype=torch.int32, device="cuda")
+    clean = torch.where(gone[:, None], torch.zeros_like(t), t)
+    for value in (float("nan"), float("inf")):
+        t[gone] = value
+        dw = gpu.topk_expert_product_vjp(x, w, offset, t, source=put(source, "int32"), k=k, want_x=False)[1]
+        want = torch.zeros_like(dw)
+        if rows:
+            there = torch.where(gone, 0, put(source, "int32")).to(torch.int32)
+            want = gpu.topk_expert_product_vjp(x, w, offset, clean, source=there, k=k, want_x=False)[1]
+        assert torch.isfinite(dw).all() and torch.equal(dw, want)
