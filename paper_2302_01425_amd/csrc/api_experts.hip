@@ -11,7 +11,8 @@ namespace {
 
 constexpr int64_t kMost = int64_t(1) << 31;
 constexpr int64_t kRowsOfLaunch = int64_t(1) << 25;      // routing: up to 64 threads each
-constexpr int64_t kTokensOfLaunch = int64_t(1) << 23;    // weighted sums: up to 256
+constexpr int64_t kTokensOfLaunch = int64_t(1) << 23;    // weighted sums: up to 256, of each slice of a row
+constexpr int64_t kSlicesOfLaunch = int64_t(1) << 15;    // (the second dimension of a grid has fewer than 2^16)
 constexpr int64_t kPairsOfLaunch = int64_t(1) << 25;     // and their gradients: up to 64
 
 int64_t size_of(int type) { return type == TOPK_TYPE_F32 ? 4 : 2; }
@@ -154,20 +155,26 @@ int topk_expert_product_vjp(const void* x, int64_t x_stride, int64_t m, const vo
 
 int topk_combine_fwd(const void* y, int64_t y_stride, const int32_t* slot, const float* val, int64_t rows, int64_t k,
                      int64_t slots, int64_t h, int type, void* out, void* stream) {
-  const topk::CombineArgs c{y, y_stride, slot, val, nullptr, 0, rows, k, slots, h, out, nullptr, nullptr};
+  const topk::CombineArgs c{y, y_stride, slot, val, nullptr, 0, rows, k, slots, h, 0, 0, out, nullptr, nullptr};
   const int rc = check_combine(c, type);
   if (rc != TOPK_OK) return rc;
   if (rows == 0) return TOPK_OK;
   if ((y == nullptr && slots > 0) || slot == nullptr || out == nullptr) return TOPK_ERR_NULL;
   begin();
+  const int64_t slices = topk::combine_slices(type, h), across = std::min(slices, kSlicesOfLaunch);
+  const int64_t tokens = kTokensOfLaunch / across;
   int launched = 0;
-  for (int64_t t = 0; t < rows && launched == 0; t += kTokensOfLaunch) {
-    topk::CombineArgs part = c;
-    part.rows = std::min(rows - t, kTokensOfLaunch);
-    part.slot = slot + t * k;
-    part.val = val == nullptr ? nullptr : val + t * k;
-    part.out = ahead(out, t * h * size_of(type));
-    launched = topk::launch_combine_fwd(type, part, as_stream(stream));
+  for (int64_t s = 0; s < slices; s += across) {
+    for (int64_t t = 0; t < rows && launched == 0; t += tokens) {
+      topk::CombineArgs part = c;
+      part.rows = std::min(rows - t, tokens);
+      part.slot = slot + t * k;
+      part.val = val == nullptr ? nullptr : val + t * k;
+      part.out = ahead(out, t * h * size_of(type));
+      part.slice = s;
+      part.slices = std::min(slices - s, across);
+      launched = topk::launch_combine_fwd(type, part, as_stream(stream));
+    }
   }
   return finish(launched);
 }
@@ -175,7 +182,7 @@ int topk_combine_fwd(const void* y, int64_t y_stride, const int32_t* slot, const
 int topk_combine_vjp(const void* y, int64_t y_stride, const int32_t* slot, const float* val, const void* cotangent,
                      int64_t cotangent_stride, int64_t rows, int64_t k, int64_t slots, int64_t h, int type, void* dy_out,
                      float* dval_out, void* stream) {
-  const topk::CombineArgs c{y, y_stride, slot, val, cotangent, cotangent_stride, rows, k, slots, h, nullptr, dy_out, dval_out};
+  const topk::CombineArgs c{y, y_stride, slot, val, cotangent, cotangent_stride, rows, k, slots, h, 0, 0, nullptr, dy_out, dval_out};
   const int rc = check_combine(c, type);
   if (rc != TOPK_OK) return rc;
   if (rows == 0) return TOPK_OK;

@@ -40,15 +40,15 @@ __device__ __forceinline__ void store_part(T* p, int64_t h, const float (&v)[N])
   }
 }
 
-// `lanes` lanes (a power of two) per token, of one workgroup: its parts are neighbours in memory; blockIdx.y: the part of a
-// row that is longer.  Two rows of y are on their way at a time (8192 x 8, 1024 columns of bfloat16: 32 us; four 36).
+// `lanes` lanes (a power of two) per token, of one workgroup: its parts are neighbours in memory; blockIdx.y: the
+// slice of a row that is longer.  Two rows of y are on their way at a time (8192 x 8, 1024 columns of bfloat16: 32 us; four 36).
 template <class T, bool SHORT>
 __global__ __launch_bounds__(kThreads) void combine_fwd_kernel(CombineArgs a, int shift) {
   constexpr int N = 16 / sizeof(T);
   constexpr int kAhead = 2;
   const int lanes = 1 << shift;
   const int64_t t = (int64_t(blockIdx.x) * kThreads + threadIdx.x) >> shift;
-  int64_t c = (int64_t(blockIdx.y) * lanes + (threadIdx.x & (lanes - 1))) * N;
+  int64_t c = ((a.slice + blockIdx.y) * lanes + (threadIdx.x & (lanes - 1))) * N;
   if (t >= a.rows || c >= a.h) return;
   c = SHORT ? 0 : min(c, a.h - N);
   const T* yp = static_cast<const T*>(a.y) + c;
@@ -142,9 +142,8 @@ template <class T>
 int fwd_type(const CombineArgs& a, hipStream_t stream) {
   const int shift = lanes_shift(a.h, sizeof(T), 8);
   const int64_t blocks = ((a.rows << shift) + kThreads - 1) / kThreads;
-  const int64_t slices = (a.h * int64_t(sizeof(T)) + (16 << shift) - 1) / (16 << shift);
-  if (!launchable(blocks * slices, kThreads) || slices > 65535) return -1;
-  const dim3 grid = dim3(unsigned(blocks), unsigned(slices)), block(kThreads);
+  if (!launchable(blocks * a.slices, kThreads) || a.slices > 65535) return -1;
+  const dim3 grid = dim3(unsigned(blocks), unsigned(a.slices)), block(kThreads);
   if (a.h * int64_t(sizeof(T)) < 16) hipLaunchKernelGGL((combine_fwd_kernel<T, true>), grid, block, 0, stream, a, shift);
   else hipLaunchKernelGGL((combine_fwd_kernel<T, false>), grid, block, 0, stream, a, shift);
   return 0;
@@ -161,6 +160,12 @@ int vjp_type(const CombineArgs& a, hipStream_t stream) {
 }
 
 }  // namespace
+
+int64_t combine_slices(int type, int64_t h) {
+  const int size = type == kF32 ? 4 : 2;
+  const int64_t bytes = int64_t(16) << lanes_shift(h, size, 8);
+  return (h * size + bytes - 1) / bytes;
+}
 
 int launch_combine_fwd(int type, const CombineArgs& a, hipStream_t stream) {
   if (type == kF32) return fwd_type<float>(a, stream);

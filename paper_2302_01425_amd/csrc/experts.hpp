@@ -86,10 +86,12 @@ struct CombineArgs {
   const void* t;             // cotangent [rows][h]
   int64_t t_stride;
   int64_t rows, k, slots, h;
+  int64_t slice, slices;     // forward: parts of a row, of a workgroup each, that a launch takes
   void* out;                 // [rows][h]
   void* dy;                  // [slots][h]
   float* dval;               // [rows][k]
 };
+int64_t combine_slices(int type, int64_t h);      // of a row
 int launch_combine_fwd(int type, const CombineArgs& a, hipStream_t stream);
 int launch_combine_vjp(int type, const CombineArgs& a, hipStream_t stream);
 

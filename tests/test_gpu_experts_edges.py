@@ -124,3 +124,20 @@ def test_weight_gradient_leaves_absent_rows_out(gpu, n, share, rows, h, ho, dtyp
             there = torch.where(gone, 0, put(source, "int32")).to(torch.int32)
             want = gpu.topk_expert_product_vjp(x, w, offset, clean, source=there, k=k, want_x=False)[1]
         assert torch.isfinite(dw).all() and torch.equal(dw, want)
+
+
+# ---- calls of several launches ---------------------------------------------------------------------------------------------
+
+# rows of `h` elements, several workgroups long, and more tokens than one launch of such workgroups has
+@pytest.mark.parametrize("dtype,rows,h", [("bfloat16", (1 << 23) + 3, 2049), ("float32", 2, 65535 * 1024 + 5), ("bfloat16", 3, 2 * 32768 * 2048 + 9)])
+def test_combine_of_long_rows_takes_several_launches(gpu, dtype, rows, h):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    y = torch.randn((5, h), generator=g, device="cuda").to(getattr(torch, dtype))
+    slot = torch.randint(-1, 5, (rows, 1), generator=g, device="cuda", dtype=torch.int32)
+    out = gpu.topk_combine_fwd(y, slot)
+    step = max(1, (1 << 31) // h)
+    for at in range(0, rows, step):
+        s = slot[at:at + step, 0]
+        want = torch.where(s[:, None] >= 0, y[s.clamp(min=0).long()], torch.zeros((), dtype=y.dtype, device="cuda"))
+        assert torch.equal(out[at:at + step], want), at
