@@ -143,6 +143,7 @@ struct RowsArgs {
   int n;
   int64_t cols, depth, col_tiles;
   void* c;
+  int64_t first = 0;       // number of the launch's first workgroup
 };
 // dW: k runs over an expert's places; one of the two operands goes through `source`
 struct WeightArgs {
@@ -158,6 +159,7 @@ struct WeightArgs {
   void* c;
   // tiles, and those of a die (split_tiles)
   int64_t m_tiles = 0, col_tiles = 0, die_m = 0, die_cols = 0;
+  int64_t first = 0;       // number of the launch's first workgroup
 };
 // Every die gets an eighth of every expert's tiles, since experts differ in their rows: a rectangle of the tiles, that of 1 x 8, 2 x
 // 4, 4 x 2 or 8 x 1 such rectangles that reads least, or an eighth of the tiles in row order (die_cols 0) where rectangles would
@@ -199,6 +201,16 @@ __device__ __forceinline__ bool find_weight_tile(const WeightArgs& g, uint32_t b
 // workgroups for all pairs: as many tiles of rows as there can be, and room for the last runs
 inline int64_t rows_blocks(const RowsArgs& g, int size) {
   return (g.slots / size + min(int64_t(g.n), g.slots)) * g.col_tiles + kDies * kRunMost;
+}
+// launch(g, grid) for workgroups 0 .. blocks - 1 of kThreads threads, in as many launches as that takes (of whole turns of the
+// dies).  Returns -1 where their numbers do not fit 32 bits.
+template <int kThreads, class ARGS, class LAUNCH>
+int in_launches(ARGS g, int64_t blocks, LAUNCH launch) {
+  constexpr int64_t kMost = (int64_t(1) << 31) / kThreads;
+  static_assert(kMost % kDies == 0, "workgroup b is on die b % kDies");
+  if (blocks >= (int64_t(1) << 32)) return -1;
+  for (g.first = 0; g.first < blocks; g.first += kMost) launch(g, dim3(unsigned(min(blocks - g.first, kMost))));
+  return 0;
 }
 
 // few rows per expert, limit > 0; W contiguous in n: of 32 columns at least

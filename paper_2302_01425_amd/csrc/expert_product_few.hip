@@ -48,7 +48,7 @@ __global__ __launch_bounds__(kThreads) void few_rows_kernel(RowsArgs g, int turn
   constexpr int kCols = KC ? kColsAlong : kColsAcross;
   __shared__ float sums[2][kWaves][kRows * kCols];
   Found f;
-  if (!find_tile<kThreads>(g.offset, g.n, g.slots, blockIdx.x, g.col_tiles, kRows, &f)) return;
+  if (!find_tile<kThreads>(g.offset, g.n, g.slots, g.first + blockIdx.x, g.col_tiles, kRows, &f)) return;
   const int lane = int(threadIdx.x) & (kWave - 1), wave = int(threadIdx.x) / kWave;
   const T* w = static_cast<const T*>(g.w) + f.expert * g.w_expert;
   // rows that are not there are read from another row, and not stored, or stored as zeros
@@ -172,12 +172,10 @@ int few_type(RowsArgs g, bool k_contiguous, hipStream_t stream) {
   }
   const int64_t cols = k_contiguous ? kColsAlong * turns : kColsAcross;
   g.col_tiles = (g.cols + cols - 1) / cols;
-  const int64_t blocks = rows_blocks(g, kRows);
-  if (!launchable(blocks, kThreads)) return -1;
-  const dim3 grid = dim3(unsigned(blocks)), block(kThreads);
-  if (k_contiguous) hipLaunchKernelGGL((few_rows_kernel<T, true>), grid, block, 0, stream, g, int(turns));
-  else hipLaunchKernelGGL((few_rows_kernel<T, false>), grid, block, 0, stream, g, int(turns));
-  return 0;
+  return in_launches<kThreads>(g, rows_blocks(g, kRows), [&](const RowsArgs& part, dim3 grid) {
+    if (k_contiguous) hipLaunchKernelGGL((few_rows_kernel<T, true>), grid, dim3(kThreads), 0, stream, part, int(turns));
+    else hipLaunchKernelGGL((few_rows_kernel<T, false>), grid, dim3(kThreads), 0, stream, part, int(turns));
+  });
 }
 
 }  // namespace

@@ -107,26 +107,25 @@ template <class T, bool B_KC>
 __global__ __launch_bounds__(kThreads, 2) void rows_large_kernel(RowsArgs g) {
   __shared__ __attribute__((aligned(1024))) char lds[2 * kStageBytes];
   Found f;
-  if (!find_tile<kThreads>(g.offset, g.n, g.slots, blockIdx.x, g.col_tiles, kRows, &f)) return;
+  if (!find_tile<kThreads>(g.offset, g.n, g.slots, g.first + blockIdx.x, g.col_tiles, kRows, &f)) return;
   if (f.end - f.begin <= kRows / 2) rows_tile<T, kRows / 2, B_KC>(g, f, lds);
   else rows_tile<T, kRows, B_KC>(g, f, lds);
 }
 
 template <class T>
-int rows_type(const RowsArgs& g, bool k_contiguous, unsigned blocks, hipStream_t stream) {
-  if (k_contiguous) hipLaunchKernelGGL((rows_large_kernel<T, true>), dim3(blocks), dim3(kThreads), 0, stream, g);
-  else hipLaunchKernelGGL((rows_large_kernel<T, false>), dim3(blocks), dim3(kThreads), 0, stream, g);
-  return 0;
+int rows_type(const RowsArgs& g, bool k_contiguous, hipStream_t stream) {
+  return in_launches<kThreads>(g, rows_blocks(g, kRows), [&](const RowsArgs& part, dim3 grid) {
+    if (k_contiguous) hipLaunchKernelGGL((rows_large_kernel<T, true>), grid, dim3(kThreads), 0, stream, part);
+    else hipLaunchKernelGGL((rows_large_kernel<T, false>), grid, dim3(kThreads), 0, stream, part);
+  });
 }
 
 }  // namespace
 
 int launch_rows_large(int type, RowsArgs g, bool k_contiguous, hipStream_t stream) {
   g.col_tiles = (g.cols + kCols - 1) / kCols;
-  const int64_t blocks = rows_blocks(g, kRows);
-  if (!launchable(blocks, kThreads)) return -1;
-  if (type == kBF16) return rows_type<bf16>(g, k_contiguous, unsigned(blocks), stream);
-  if (type == kF16) return rows_type<f16>(g, k_contiguous, unsigned(blocks), stream);
+  if (type == kBF16) return rows_type<bf16>(g, k_contiguous, stream);
+  if (type == kF16) return rows_type<f16>(g, k_contiguous, stream);
   return -1;
 }
 

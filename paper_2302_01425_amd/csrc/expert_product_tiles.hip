@@ -155,7 +155,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_tiles_kernel(RowsArgs g) {
   using T = typename TILE::T;
   __shared__ __attribute__((aligned(1024))) char lds[2 * TILE::kStageBytes];
   Found f;
-  if (!find_tile<kThreads>(g.offset, g.n, g.slots, blockIdx.x, g.col_tiles, TILE::kRows, &f)) return;
+  if (!find_tile<kThreads>(g.offset, g.n, g.slots, g.first + blockIdx.x, g.col_tiles, TILE::kRows, &f)) return;
   using IA = typename TILE::template A<true>;
   using IB = typename TILE::template B<B_KC>;
   const int64_t n0 = tile_start(f.col, TILE::kCols, g.cols);
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(kThreads, 2) void weight_tiles_kernel(WeightArgs g)
   __shared__ uint32_t there[LIST != 0 ? kTable / 32 : 1];
   int e;
   int64_t m0, n0;
-  if (!find_weight_tile(g, blockIdx.x, &e, &m0, &n0)) return;
+  if (!find_weight_tile(g, uint32_t(g.first) + blockIdx.x, &e, &m0, &n0)) return;
   int64_t begin, end;
   places(g.offset, e, g.slots, &begin, &end);
   T* c = static_cast<T*>(g.c) + e * g.m * g.cols;
@@ -214,23 +214,21 @@ __global__ __launch_bounds__(kThreads, 2) void weight_tiles_kernel(WeightArgs g)
 template <class TILE, bool TINY>
 int rows_tile(RowsArgs g, bool k_contiguous, hipStream_t stream) {
   g.col_tiles = (g.cols + TILE::kCols - 1) / TILE::kCols;
-  const int64_t blocks = rows_blocks(g, TILE::kRows);
-  if (!launchable(blocks, kThreads)) return -1;
-  const dim3 grid = dim3(unsigned(blocks)), block(kThreads);
-  if (k_contiguous) hipLaunchKernelGGL((rows_tiles_kernel<TILE, true, TINY>), grid, block, 0, stream, g);
-  else hipLaunchKernelGGL((rows_tiles_kernel<TILE, false, TINY>), grid, block, 0, stream, g);
-  return 0;
+  return in_launches<kThreads>(g, rows_blocks(g, TILE::kRows), [&](const RowsArgs& part, dim3 grid) {
+    if (k_contiguous) hipLaunchKernelGGL((rows_tiles_kernel<TILE, true, TINY>), grid, dim3(kThreads), 0, stream, part);
+    else hipLaunchKernelGGL((rows_tiles_kernel<TILE, false, TINY>), grid, dim3(kThreads), 0, stream, part);
+  });
 }
 
 template <class TILE, Load LOAD>
 int weight_tile(WeightArgs g, hipStream_t stream) {
   const int64_t blocks = split_tiles(&g, TILE::kRows, TILE::kCols);
-  if (!launchable(blocks, kThreads)) return -1;
-  const dim3 grid = dim3(unsigned(blocks)), block(kThreads);
-  if (g.a_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 1, LOAD>), grid, block, 0, stream, g);
-  else if (g.b_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 2, LOAD>), grid, block, 0, stream, g);
-  else hipLaunchKernelGGL((weight_tiles_kernel<TILE, 0, LOAD>), grid, block, 0, stream, g);
-  return 0;
+  return in_launches<kThreads>(g, blocks, [&](const WeightArgs& part, dim3 grid) {
+    const dim3 block(kThreads);
+    if (part.a_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 1, LOAD>), grid, block, 0, stream, part);
+    else if (part.b_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 2, LOAD>), grid, block, 0, stream, part);
+    else hipLaunchKernelGGL((weight_tiles_kernel<TILE, 0, LOAD>), grid, block, 0, stream, part);
+  });
 }
 template <class T>
 int rows_type(const RowsArgs& g, bool k_contiguous, TileKind kind, hipStream_t stream) {

@@ -141,3 +141,30 @@ def test_combine_of_long_rows_takes_several_launches(gpu, dtype, rows, h):
         s = slot[at:at + step, 0]
         want = torch.where(s[:, None] >= 0, y[s.clamp(min=0).long()], torch.zeros((), dtype=y.dtype, device="cuda"))
         assert torch.equal(out[at:at + step], want), at
+
+
+def test_products_of_more_tiles_than_a_launch_takes(gpu):
+    import torch
+    slots = (1 << 30) + 70
+    x = torch.randn((slots, 1), device="cuda")
+    w = torch.tensor([2.0, -0.5], device="cuda").view(2, 1, 1)
+    half = slots // 2 + 5
+    offset = torch.tensor([0, half, slots], dtype=torch.int32, device="cuda")
+    out = gpu.topk_expert_product_fwd(x, w, offset)
+    assert torch.equal(out[:half], 2.0 * x[:half]) and torch.equal(out[half:], -0.5 * x[half:])
+    del out, x
+    n, h = 1024, (1 << 20) + 9
+    x, t = torch.randn((5, h), device="cuda"), torch.randn((5, 1), device="cuda")
+    offset = torch.full((n + 1,), 5, dtype=torch.int32, device="cuda")
+    offset[:3], offset[3:n] = torch.tensor([0, 0, 2]), 4                     # experts 1, 2 and the last have places
+    w = torch.zeros((1, 1, h), device="cuda").expand(n, 1, h)
+    _, dw = gpu.topk_expert_product_vjp(x, w, offset, t, want_x=False)
+    at = offset.tolist()
+    for e in range(n):
+        if at[e] == at[e + 1]:
+            assert (dw[e] == 0).all(), e
+        else:
+            part = slice(at[e], at[e + 1])
+            terms = t[part].double() * x[part].double()
+            # two products and their sum, rounded
+            assert ((dw[e, 0].double() - terms.sum(dim=0)).abs() <= 3 * 2.0 ** -24 * terms.abs().sum(dim=0)).all(), e
