@@ -101,7 +101,7 @@ struct Table {
 // 16 bytes per lane from `from` to LDS at `to` (the same for the wavefront) + 16 * lane.  Not waited for, and unknown to the
 // compiler's own waits: wait_stage() counts these loads.
 __device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory", "m0");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(to) : "memory");
 }
 // all loads to LDS but the last LEFT of this wavefront have arrived, all its accesses of LDS are done, and so for every
 // wavefront
