@@ -55,13 +55,13 @@ int launch_rows(int type, const RowsArgs& g, bool k_contiguous, hipStream_t stre
 
 int launch_product_fwd(int type, const ProductArgs& p, hipStream_t stream) {
   RowsArgs g{p.x, p.x_stride, p.source, divisor(p.k), p.m, p.w, p.w_expert, p.w_in == 1 ? p.w_out : p.w_in, p.offset, p.slots,
-             p.n, p.ho, p.h, 0, p.out};
+             p.n, 0, p.ho, p.h, 0, p.out};
   return launch_rows(type, g, p.w_in == 1, stream);
 }
 
 int launch_product_dx(int type, const ProductArgs& p, hipStream_t stream) {
   RowsArgs g{p.t, p.t_stride, nullptr, Divisor{}, p.slots, p.w, p.w_expert, p.w_out == 1 ? p.w_in : p.w_out, p.offset, p.slots,
-             p.n, p.h, p.ho, 0, p.dx};
+             p.n, 0, p.h, p.ho, 0, p.dx};
   return launch_rows(type, g, p.w_out == 1, stream);
 }
 
@@ -69,10 +69,10 @@ int launch_product_dw(int type, const ProductArgs& p, hipStream_t stream) {
   // dW has the layout of w: its contiguous direction gives the columns
   WeightArgs g;
   if (p.w_in == 1)
-    g = {p.t, p.x, p.t_stride, p.x_stride, nullptr, p.source, divisor(p.k), p.slots, p.m, p.offset, p.slots, p.n, p.ho, p.h,
+    g = {p.t, p.x, p.t_stride, p.x_stride, nullptr, p.source, divisor(p.k), p.slots, p.m, p.offset, p.slots, p.n, 0, p.ho, p.h,
          p.dw};
   else
-    g = {p.x, p.t, p.x_stride, p.t_stride, p.source, nullptr, divisor(p.k), p.m, p.slots, p.offset, p.slots, p.n, p.h, p.ho,
+    g = {p.x, p.t, p.x_stride, p.t_stride, p.source, nullptr, divisor(p.k), p.m, p.slots, p.offset, p.slots, p.n, 0, p.h, p.ho,
          p.dw};
   const int s = size_of(type);
   const bool whole = whole_parts(g.a, g.a_stride, g.m, s) && whole_parts(g.b, g.b_stride, g.cols, s) &&

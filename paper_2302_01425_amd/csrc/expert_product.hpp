@@ -129,7 +129,8 @@ __device__ __forceinline__ bool find_tile(const int32_t* offset, int n, int64_t 
   return f->expert >= 0;
 }
 
-// forward and dx: rows of A are places, B is W[e] seen as [n][k] (contiguous in k or in n)
+// forward and dx: rows of A are places, B is W[e] seen as [n][k] (contiguous in k or in n).  With what a kernel takes beside it, 128
+// bytes: arguments of one more line cost the smallest calls 0.3 to 0.5 us.
 struct RowsArgs {
   const void* a;
   int64_t a_stride;
@@ -141,10 +142,11 @@ struct RowsArgs {
   const int32_t* offset;
   int64_t slots;
   int n;
+  uint32_t first;          // number of the launch's first workgroup
   int64_t cols, depth, col_tiles;
   void* c;
-  int64_t first = 0;       // number of the launch's first workgroup
 };
+static_assert(sizeof(RowsArgs) + sizeof(int) <= 128, "two lines of arguments");
 // dW: k runs over an expert's places; one of the two operands goes through `source`
 struct WeightArgs {
   const void *a, *b;
@@ -155,11 +157,11 @@ struct WeightArgs {
   const int32_t* offset;
   int64_t slots;
   int n;
+  uint32_t first;          // number of the launch's first workgroup
   int64_t m, cols;
   void* c;
   // tiles, and those of a die (split_tiles)
   int64_t m_tiles = 0, col_tiles = 0, die_m = 0, die_cols = 0;
-  int64_t first = 0;       // number of the launch's first workgroup
 };
 // Every die gets an eighth of every expert's tiles, since experts differ in their rows: a rectangle of the tiles, that of 1 x 8, 2 x
 // 4, 4 x 2 or 8 x 1 such rectangles that reads least, or an eighth of the tiles in row order (die_cols 0) where rectangles would
@@ -209,7 +211,10 @@ int in_launches(ARGS g, int64_t blocks, LAUNCH launch) {
   constexpr int64_t kMost = (int64_t(1) << 31) / kThreads;
   static_assert(kMost % kDies == 0, "workgroup b is on die b % kDies");
   if (blocks >= (int64_t(1) << 32)) return -1;
-  for (g.first = 0; g.first < blocks; g.first += kMost) launch(g, dim3(unsigned(min(blocks - g.first, kMost))));
+  for (int64_t b = 0; b < blocks; b += kMost) {
+    g.first = uint32_t(b);
+    launch(g, dim3(unsigned(min(blocks - b, kMost))));
+  }
   return 0;
 }
 

@@ -182,7 +182,7 @@ __global__ __launch_bounds__(kThreads, 2) void weight_tiles_kernel(WeightArgs g)
   __shared__ uint32_t there[LIST != 0 ? kTable / 32 : 1];
   int e;
   int64_t m0, n0;
-  if (!find_weight_tile(g, uint32_t(g.first) + blockIdx.x, &e, &m0, &n0)) return;
+  if (!find_weight_tile(g, g.first + blockIdx.x, &e, &m0, &n0)) return;
   int64_t begin, end;
   places(g.offset, e, g.slots, &begin, &end);
   T* c = static_cast<T*>(g.c) + e * g.m * g.cols;
