@@ -413,7 +413,8 @@ int topk_combine_fwd(const void* y, int64_t y_stride, const int32_t* slot, const
 /*
  * Its gradients: dy_out[slot[t][j]] = val[t][j] cotangent[t], rows that no pair names left as they were;
  * dval_out[t][j] = <cotangent[t], y[slot[t][j]]>, 0 for an empty place (NULL with val NULL: not wanted; y may be NULL then).
- * A place is named by one pair at most, as topk_expert_map gives them (where two name it, dy_out there is one of theirs).
+ * A place is named by one pair at most, as topk_expert_map gives them (where two name it, every element of dy_out there is one of
+ * theirs).
  *   cotangent [rows][h]; dy_out [slots][h] contiguous; dval_out [rows][k].
  */
 int topk_combine_vjp(const void* y, int64_t y_stride, const int32_t* slot, const float* val, const void* cotangent,

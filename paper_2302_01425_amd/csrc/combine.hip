@@ -2,7 +2,7 @@
 //   out[t] = sum_j val[t][j] y[slot[t][j]];   dy[slot[t][j]] = val[t][j] dout[t],  dval[t][j] = <dout[t], y[slot[t][j]]>
 // Places outside [0, slots) are left out (dval 0).  Sums in float32, one rounding per output.  Bound by HBM: every row of y
 // is read once (vjp: and a row of dy written), every row of out written (dout read) once.  16384 x 2 rows of 2048 bfloat16: 41 us,
-// 4.9 TB/s; gradient of 8191 x 8 rows of 1001 float16: 69 us, 4.0 TB/s (a row of an odd number of elements begins inside a line).
+// 4.9 TB/s; gradient of 8191 x 8 rows of 1001 float16: 74 us, 3.8 TB/s (a row of an odd number of elements begins inside a line).
 #include "common.hpp"
 #include "experts.hpp"
 

@@ -6,7 +6,7 @@
 // there (for float32 that costs more than the loads), and no LDS images: a row of W is used by one workgroup.
 //
 // Bound by HBM and, for the smallest calls, by the launch and the search of the expert (5 us).  One token to two of 8 experts, W not in
-// a cache, 2048 -> 4096: bfloat16 10.9 us, 3.1 TB/s, dx 12.9; float32 16.2 us, 4.1 TB/s, dx 27.9.
+// a cache, 2048 -> 4096: bfloat16 11.3 us, 3.0 TB/s, dx 12.9; float32 16.8 us, 4.0 TB/s, dx 28.1.
 #include "expert_product.hpp"
 
 namespace topk {

@@ -4,13 +4,13 @@
 // A workgroup of eight wavefronts holds the tile's float32 sums in registers, 128 x 64 per wavefront: 12 fragments of 1 KB read
 // from LDS feed 32 matrix instructions.  A step is 128 bytes of k (whole cache lines of rows that are contiguous in k), 64 KB
 // of LDS for both operands, and lies in two halves: the fragments of a half are read while the other half is multiplied, and
-// the loads of the step after the next are issued one by one between the second half's instructions (in a run before them:
-// 354 us for 327 below).  The last tile of an expert's rows is one of 128 rows where it has no more.
+// the loads of the step after the next are issued one by one between the second half's instructions (in a run before them
+// they cost 8 % more).  The last tile of an expert's rows is one of 128 rows where it has no more.
 //
-// Bound by the loads of a step and the instructions beside the matrix ones, not by LDS (no bank conflicts; at 8192 tokens x 2,
-// 2 experts, 2048 -> 4096 the matrix units are busy half of the time, the wavefronts wait for loads a third).  bfloat16: one
-// expert of 8192 rows, 8192 -> 8192: 955 us, 1.15 PFLOP/s; 8192 tokens x 2 to 32 experts of unequal shares, 2048 -> 4096: 330 us
-// forward, 325 us dx, 0.84 PFLOP/s with a seventh of the multiplied rows empty.
+// Bound by the distance between a step's loads and their use, not by LDS (no bank conflicts): at 8192 tokens x 2 to 32 experts of
+// unequal shares, 2048 -> 4096, the matrix units are busy 43 % of the time and the wavefronts wait 40 % of theirs; bfloat16, forward
+// 338 us, dx 336, 0.81 PFLOP/s with a seventh of the multiplied rows empty.  One expert of 8192 rows, 8192 -> 8192: 950 to 990 us, 1.11
+// to 1.16 PFLOP/s.
 #include "expert_tiles.hpp"
 
 namespace topk {

@@ -9,7 +9,8 @@
 // any alignment: operands pass through registers, two steps ahead, to two images; two and four workgroups share a compute
 // unit.  Small is for float32, whose matrix instructions take 16 times as long for the same fragments, and where larger tiles
 // would leave compute units without work.  What binds the others is the first cache: 16 bytes at any address take twice the
-// time of aligned ones (8192 tokens x 2, 8 experts, 2001 -> 3001, bfloat16: 388 us, without the loads 178).
+// time of aligned ones (8192 tokens x 2, 8 experts, 2001 -> 3001, bfloat16: 411 us, less than half of that
+// without the loads).
 #include "expert_tiles.hpp"
 
 namespace topk {

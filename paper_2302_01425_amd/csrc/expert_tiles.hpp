@@ -99,7 +99,7 @@ struct Table {
 };
 
 // 16 bytes per lane from `from` to LDS at `to` (the same for the wavefront) + 16 * lane.  Not waited for, and unknown to the
-// compiler's own waits: wait_stage() counts these loads.
+// compiler's own waits: wait_stage() counts these loads.  (The hardware takes `to` from m0; one instruction has to lie between.)
 __device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(to) : "memory");
 }

@@ -8,8 +8,8 @@
 //
 // A row lies in the registers of 8 to 64 lanes and is read once; k rounds take the largest each.  Bound by the launch below some
 // 1000 rows (5 us a call), by instructions above: a round of 32 lanes x 8 elements is 87 of them.  16384 x 64 float32, softmax, k = 2:
-// 4.2 us, 1.0 TB/s; 8192 x 256 bfloat16, sigmoid, bias, 8 groups, k = 8: 12.5 us a call, 0.38 TB/s (16 lanes x 16 elements: 12 to
-// 17 us, and 2 us more for few rows).
+// 4.4 us, 1.0 TB/s; 8192 x 256 bfloat16, sigmoid, bias, 8 groups, k = 8: 12.5 and 13.5 us a call (two draws of the inputs), 0.38 and
+// 0.35 TB/s (16 lanes x 16 elements: 12 to 17 us, and 2 us more for few rows).
 #include <cmath>
 
 #include "experts.hpp"
@@ -372,7 +372,8 @@ __global__ __launch_bounds__(kThreads) void route_fwd_kernel(RouteArgs a, int la
 //   sigmoid, renormalised   dl[idx_j] += scale w_j (1 - s_j) (t_j - mean)
 //   sigmoid                 dl[idx_j] += scale s_j (1 - s_j) t_j
 // Lane q of a row takes the choices q, q + GL, ..: their terms are then handed to the lanes that hold the entries.  Only
-// softmax that is not renormalised reads the whole row.  All of the gradient is written: 32768 x 128 float32, k = 8: 12 us, 2.9 TB/s.
+// softmax that is not renormalised reads the whole row.  All of the gradient is written: 32768 x 128 float32, k = 8: 12.6 us
+// a call, 2.8 TB/s; the others 9.9 (softmax), 10.6 and 9.8 (sigmoid), 2.0 TB/s.
 template <class T, int GL, int E>
 __global__ __launch_bounds__(kThreads) void route_vjp_kernel(RouteVjpArgs a) {
   constexpr int J = kChoicesMax / GL;                              // choices of a lane, at most
