@@ -421,6 +421,68 @@ int topk_combine_vjp(const void* y, int64_t y_stride, const int32_t* slot, const
                      int64_t cotangent_stride, int64_t rows, int64_t k, int64_t slots, int64_t h, int type, void* dy_out,
                      float* dval_out, void* stream);
 
+/*
+ * ---- The experts' feed-forward ---------------------------------------------------------------------------------------
+ *
+ * What an expert does with its rows: the gated block (two projections, the activation, the product) with its gradients, and for
+ * serving products in 8-bit integers.  Places, lists, strides, types and the checks on the device are those above; the last
+ * product of a block is topk_expert_product_fwd (rows in expert order).  One expert with offset = (0, rows) is a dense block.
+ */
+/* act(g): g / (1 + exp(-g)); g Phi(g), Phi the normal distribution; g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2; max(g, 0) */
+enum { TOPK_ACT_SILU = 0, TOPK_ACT_GELU = 1, TOPK_ACT_GELU_TANH = 2, TOPK_ACT_RELU = 3 };
+#define TOPK_I8_WIDTH_MAX 131071    /* terms of a sum of 8-bit products, which is exact in int32 */
+
+/*
+ * The gated block.  For every place s of expert e, with g = W_gate[e] x[r(s)] and u = W_up[e] x[r(s)]: out[s] = act(g) u.
+ *   w_gate, w_up: [n][f][h] of `type` as w of topk_expert_product_fwd, both with the same strides (two arrays, or two parts of
+ *   one); out [slots][f]; pre_out [slots][2][f] receives g and u, rounded to `type`, for topk_expert_gated_vjp (may be NULL).
+ *   Rows of out and pre_out behind offset[n] are left as they were; a place whose source is out of range has rows of zeros.
+ */
+int topk_expert_gated_fwd(const void* x, int64_t x_stride, int64_t m, const void* w_gate, const void* w_up, int64_t w_expert,
+                          int64_t w_out, int64_t w_in, const int32_t* offset, const int32_t* source, int64_t k, int64_t slots,
+                          int64_t n, int64_t h, int64_t f, int type, int act, void* out, void* pre_out, void* stream);
+
+/*
+ * Its gradients.  dg = cotangent u act'(g), du = cotangent act(g), both rounded to `type` (act' of TOPK_ACT_RELU is 0 at 0);
+ * dx_out[s] = W_gate[e]^T dg[s] + W_up[e]^T du[s], per PLACE as topk_expert_product_vjp (zeros where the source is out of range);
+ * dw_gate_out[e] = sum over e's places of dg[s] x[r(s)]^T, dw_up_out[e] likewise with du, zeros for an expert without places.
+ *   pre: pre_out of the forward pass; with NULL g and u are computed again, in float32.  Either dx_out or both dw_*_out may be
+ *   NULL.  cotangent [slots][f]; dw_*_out contiguous as dw_out of topk_expert_product_vjp.  scratch:
+ *   topk_expert_gated_vjp_bytes(slots, f, type) bytes of the caller's for this call (TOPK_ERR_WORKSPACE if smaller), 16-byte
+ *   aligned; calls that may overlap need one each.
+ */
+size_t topk_expert_gated_vjp_bytes(int64_t slots, int64_t f, int type);
+int topk_expert_gated_vjp(const void* x, int64_t x_stride, int64_t m, const void* w_gate, const void* w_up, int64_t w_expert,
+                          int64_t w_out, int64_t w_in, const int32_t* offset, const int32_t* source, int64_t k, int64_t slots,
+                          int64_t n, int64_t h, int64_t f, int type, int act, const void* pre, const void* cotangent,
+                          int64_t cotangent_stride, void* dx_out, void* dw_gate_out, void* dw_up_out, void* scratch,
+                          size_t scratch_bytes, void* stream);
+
+/*
+ * Rows in 8 bits, tokens of activations or channels of weights (the rows of an [n * out][in] array): scale_out = max |x| / 127,
+ * q_out = 127 x / max |x| rounded to the nearest integer, ties to even (of the exact quotient).  A row of zeros has scale 0; a
+ * row that holds an infinity or NaN has scale NaN and zeros, so that what is made of it is NaN.
+ *   x [m][h] of `type`, x_stride between rows; q_out [m][h] int8, scale_out [m].
+ */
+int topk_quantise_rows(const void* x, int64_t x_stride, int64_t m, int64_t h, int type, int8_t* q_out, float* scale_out,
+                       void* stream);
+
+/*
+ * The experts' products of 8-bit integers: out[s][o] = x_scale[r(s)] w_scale[e][o] sum_i w(e, o, i) x[r(s)][i], the sum exact.
+ *   x [m][h] int8, x_stride between rows; x_scale [m]; w(e, o, i) int8 at w[e * w_expert + o * w_out + i]; w_scale [n][ho];
+ *   1 <= h <= TOPK_I8_WIDTH_MAX; out [slots][ho] of out_type.  Otherwise as topk_expert_product_fwd.
+ */
+int topk_expert_product_i8_fwd(const int8_t* x, int64_t x_stride, int64_t m, const float* x_scale, const int8_t* w,
+                               int64_t w_expert, int64_t w_out, const float* w_scale, const int32_t* offset,
+                               const int32_t* source, int64_t k, int64_t slots, int64_t n, int64_t h, int64_t ho, int out_type,
+                               void* out, void* stream);
+
+/* The gated block of 8-bit integers: topk_expert_gated_fwd with g and u such products.  Both weights have the same strides. */
+int topk_expert_gated_i8_fwd(const int8_t* x, int64_t x_stride, int64_t m, const float* x_scale, const int8_t* w_gate,
+                             const float* gate_scale, const int8_t* w_up, const float* up_scale, int64_t w_expert, int64_t w_out,
+                             const int32_t* offset, const int32_t* source, int64_t k, int64_t slots, int64_t n, int64_t h,
+                             int64_t f, int out_type, int act, void* out, void* stream);
+
 /* Static, human-readable text for a return code. */
 const char* topk_strerror(int code);
 

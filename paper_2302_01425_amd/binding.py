@@ -27,6 +27,8 @@ EXPORTS = (
     "topk_set_route", "topk_strerror", "topk_mask_jvp_static",
     "topk_route_fwd", "topk_route_vjp", "topk_expert_map", "topk_expert_map_bytes", "topk_expert_product_fwd",
     "topk_expert_product_vjp", "topk_combine_fwd", "topk_combine_vjp",
+    "topk_expert_gated_fwd", "topk_expert_gated_vjp", "topk_expert_gated_vjp_bytes", "topk_quantise_rows",
+    "topk_expert_product_i8_fwd", "topk_expert_gated_i8_fwd",
 )
 
 _lib = None
@@ -85,8 +87,18 @@ def load() -> ctypes.CDLL:
     L.topk_expert_product_vjp.argtypes = product + [vp, i64, vp, vp, vp]
     L.topk_combine_fwd.argtypes = [vp, i64, vp, vp, i64, i64, i64, i64, ci, vp, vp]
     L.topk_combine_vjp.argtypes = [vp, i64, vp, vp, vp, i64, i64, i64, i64, i64, ci, vp, vp, vp]
+    gated = [vp, i64, i64, vp, vp, i64, i64, i64, vp, vp, i64, i64, i64, i64, i64, ci, ci]
+    L.topk_expert_gated_fwd.argtypes = gated + [vp, vp, vp]
+    L.topk_expert_gated_vjp.argtypes = gated + [vp, vp, i64, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    L.topk_expert_gated_vjp_bytes.argtypes = [i64, i64, ci]
+    L.topk_expert_gated_vjp_bytes.restype = ctypes.c_size_t
+    L.topk_quantise_rows.argtypes = [vp, i64, i64, i64, ci, vp, vp, vp]
+    L.topk_expert_product_i8_fwd.argtypes = [vp, i64, i64, vp, vp, i64, i64, vp, vp, vp, i64, i64, i64, i64, i64, ci, vp, vp]
+    L.topk_expert_gated_i8_fwd.argtypes = [vp, i64, i64, vp, vp, vp, vp, vp, i64, i64, vp, vp, i64, i64, i64, i64, i64, ci, ci,
+                                           vp, vp]
     for name in ("topk_route_fwd", "topk_route_vjp", "topk_expert_map", "topk_expert_product_fwd",
-                 "topk_expert_product_vjp", "topk_combine_fwd", "topk_combine_vjp"):
+                 "topk_expert_product_vjp", "topk_combine_fwd", "topk_combine_vjp", "topk_expert_gated_fwd",
+                 "topk_expert_gated_vjp", "topk_quantise_rows", "topk_expert_product_i8_fwd", "topk_expert_gated_i8_fwd"):
         getattr(L, name).restype = ci
     L.topk_workspace_bytes.argtypes = [ci, i64, i64, i64, dbl]
     L.topk_workspace_bytes.restype = ctypes.c_size_t
@@ -864,3 +876,183 @@ def topk_combine_vjp(y, slot, val, cotangent, dy_out=None, dval_out=None, stream
             None if dval is None else dval.data_ptr(), st), "topk_combine_vjp")
         return dy, dval
     return _on(y, stream, call)
+
+
+# ---- the experts' feed-forward: the gated block with its gradients, and products in 8-bit integers ------------------------
+# Lists, types, strides, devices and streams as above.
+TOPK_ACT_SILU, TOPK_ACT_GELU, TOPK_ACT_GELU_TANH, TOPK_ACT_RELU = range(4)
+TOPK_I8_WIDTH_MAX = 131071
+
+
+def _lists(offset, source, n, x):
+    """Checked lists of places: their number, and the lists' addresses."""
+    _exact(offset, (n + 1,), torch.int32, x, "offset")
+    if source is None:
+        return x.shape[0], offset.data_ptr(), None
+    if not isinstance(source, torch.Tensor) or source.dim() != 1:
+        raise TopkError("source must be a 1-D int32 tensor")
+    _exact(source, source.shape, torch.int32, x, "source")
+    return source.shape[0], offset.data_ptr(), source.data_ptr()
+
+
+def _pair(w, w_up, x, dtype, name, name_up):
+    """Two arrays of weights [n, out, in] of the same layout: shape, strides (1 along a dimension of one element that could be
+    the contiguous one)."""
+    for t, what in ((w, name), (w_up, name_up)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.dtype != dtype or t.get_device() != x.get_device() or \
+                t.shape[2] != x.shape[1]:
+            raise TopkError(f"{what} must be a {dtype} tensor [n, out, {x.shape[1]}] on {x.device}")
+    if w.shape != w_up.shape or any(n > 1 and a != b for n, a, b in zip(w.shape, w.stride(), w_up.stride())):
+        raise TopkError(f"{name} and {name_up} must have the same shape and strides")
+    w_expert, w_out, w_in = w.stride()
+    if w.shape[2] == 1:
+        w_in = 1
+    elif w.shape[1] == 1 and w_in != 1:
+        w_out = 1
+    if w_in != 1 and w_out != 1:
+        raise TopkError(f"{name} must be contiguous along its last dimension or the one before it")
+    return w.shape, (w_expert, w_out, w_in)
+
+
+def _gated(x, w_gate, w_up, offset, source, k, act):
+    """Checked arguments of the gated block: what the library takes, and the shapes."""
+    x = _rows(x, "x")
+    (n, f, h), strides = _pair(w_gate, w_up, x, x.dtype, "w_gate", "w_up")
+    slots, off, src = _lists(offset, source, n, x)
+    args = (x.data_ptr(), x.stride(0), x.shape[0], w_gate.data_ptr(), w_up.data_ptr(), *strides, off, src, int(k), slots, n, h, f,
+            _TYPES[x.dtype], int(act))
+    return x, slots, n, f, h, strides[2] == 1, args
+
+
+def topk_expert_gated_fwd(x, w_gate, w_up, offset, source=None, k=1, act=TOPK_ACT_SILU, want_pre=False, out=None, pre_out=None,
+                          stream=None):
+    """Returns out [slots, f]: act(W_gate[e] x[r]) * (W_up[e] x[r]) for every place, r as in topk_expert_product_fwd, both weights
+    [n, f, h]; with want_pre (or pre_out) (out, pre), pre [slots, 2, f] both sums for topk_expert_gated_vjp.  Rows behind
+    offset[n] are not written."""
+    x, slots, n, f, h, _, args = _gated(x, w_gate, w_up, offset, source, k, act)
+    for t, shape, name in ((out, (slots, f), "out"), (pre_out, (slots, 2, f), "pre_out")):
+        if t is not None:
+            _exact(t, shape, x.dtype, x, name)
+    if out is not None or pre_out is not None:
+        _apart((("out", out), ("pre_out", pre_out)), (x, w_gate, w_up, offset, source))
+
+    def call(st):
+        y = _new(out, (slots, f), x.dtype, x)
+        pre = _new(pre_out, (slots, 2, f), x.dtype, x) if want_pre or pre_out is not None else None
+        _check((_lib or load()).topk_expert_gated_fwd(*args, y.data_ptr(), None if pre is None else pre.data_ptr(), st),
+               "topk_expert_gated_fwd")
+        return y if pre is None else (y, pre)
+    return _on(x, stream, call)
+
+
+def topk_expert_gated_vjp(x, w_gate, w_up, offset, cotangent, source=None, k=1, act=TOPK_ACT_SILU, pre=None, want_x=True,
+                          want_w=True, dx_out=None, dw_gate_out=None, dw_up_out=None, stream=None):
+    """Returns (dx [slots, h] per place, dw_gate, dw_up like the weights); what is not wanted is None.  pre: what the forward pass
+    returned with want_pre; without it both projections are computed again.  Rows of dx behind offset[n] are not written; with
+    source, topk_combine_fwd(dx, slot) gives the gradient of x."""
+    x, slots, n, f, h, plain, args = _gated(x, w_gate, w_up, offset, source, k, act)
+    cotangent = _rows(cotangent, "cotangent", x)
+    if tuple(cotangent.shape) != (slots, f):
+        raise TopkError(f"cotangent must have the shape {(slots, f)} (got {tuple(cotangent.shape)})")
+    if pre is not None:
+        _exact(pre, (slots, 2, f), x.dtype, x, "pre")
+    if dx_out is not None:
+        _exact(dx_out, (slots, h), x.dtype, x, "dx_out")
+    given = (("dw_gate_out", dw_gate_out), ("dw_up_out", dw_up_out))
+    for name, t in given:
+        if t is not None:
+            like = t if plain or not isinstance(t, torch.Tensor) or t.dim() != 3 else t.transpose(1, 2)
+            _exact(like, (n, f, h) if plain else (n, h, f), x.dtype, x, name if plain else f"{name}, transposed like the weights,")
+    if dx_out is not None or dw_gate_out is not None or dw_up_out is not None:
+        _apart((("dx_out", dx_out), *given), (x, w_gate, w_up, offset, source, cotangent, pre))
+
+    def call(st):
+        L = _lib or load()
+        dx = _new(dx_out, (slots, h), x.dtype, x) if want_x or dx_out is not None else None
+        dws = [None, None]
+        if want_w or dw_gate_out is not None or dw_up_out is not None:
+            dws = [t if t is not None else _new(None, (n, f, h), x.dtype, x) if plain
+                   else _new(None, (n, h, f), x.dtype, x).transpose(1, 2) for _, t in given]
+        if dx is None and dws[0] is None:
+            return None, None, None
+        need = L.topk_expert_gated_vjp_bytes(slots, f, _TYPES[x.dtype])
+        scratch = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+        _check(L.topk_expert_gated_vjp(
+            *args, None if pre is None else pre.data_ptr(), cotangent.data_ptr(), cotangent.stride(0),
+            *(None if t is None else t.data_ptr() for t in (dx, *dws, scratch)), need, st), "topk_expert_gated_vjp")
+        return dx, dws[0], dws[1]
+    return _on(x, stream, call)
+
+
+def topk_quantise_rows(x, q_out=None, scale_out=None, stream=None):
+    """Returns (q [m, h] int8, scale [m] float32) with x about q * scale per row: tokens, or weights seen as [n * out, in]."""
+    x = _rows(x, "x")
+    m, h = x.shape
+    for t, shape, dtype, name in ((q_out, (m, h), torch.int8, "q_out"), (scale_out, (m,), _F32, "scale_out")):
+        if t is not None:
+            _exact(t, shape, dtype, x, name)
+    if q_out is not None or scale_out is not None:
+        _apart((("q_out", q_out), ("scale_out", scale_out)), (x,))
+
+    def call(st):
+        q = _new(q_out, (m, h), torch.int8, x)
+        scale = _new(scale_out, (m,), _F32, x)
+        _check((_lib or load()).topk_quantise_rows(x.data_ptr(), x.stride(0), m, h, _TYPES[x.dtype], q.data_ptr(),
+                                                   scale.data_ptr(), st), "topk_quantise_rows")
+        return q, scale
+    return _on(x, stream, call)
+
+
+def _eight(q, q_scale, w, w_scale, w_up, up_scale, offset, source, dtype):
+    """Checked arguments of the products in 8 bits: shapes, strides of the weights, the lists."""
+    if not isinstance(q, torch.Tensor) or not q.is_cuda:
+        raise TopkError("q must be a tensor in GPU memory")
+    if q.dim() != 2 or q.dtype != torch.int8 or (q.shape[1] > 1 and q.stride(1) != 1):
+        raise TopkError("q must be a 2-D int8 tensor with contiguous rows")
+    names = ("w", "w_scale") if w_up is None else ("w_gate", "gate_scale")
+    (n, f, h), strides = _pair(w, w if w_up is None else w_up, q, torch.int8, names[0], "w_up")
+    if h > 1 and strides[2] != 1:
+        raise TopkError(f"{names[0]} must be contiguous along its last dimension")
+    _exact(q_scale, (q.shape[0],), _F32, q, "q_scale")
+    _exact(w_scale, (n, f), _F32, q, names[1])
+    if w_up is not None:
+        _exact(up_scale, (n, f), _F32, q, "up_scale")
+    if dtype not in _TYPES:
+        raise TopkError("dtype must be torch.float32, torch.bfloat16 or torch.float16")
+    return n, f, h, strides, _lists(offset, source, n, q)
+
+
+def topk_expert_product_i8_fwd(q, q_scale, w, w_scale, offset, source=None, k=1, dtype=torch.bfloat16, out=None, stream=None):
+    """Returns out [slots, ho] of dtype: q_scale[r] * w_scale[e] * (W[e] q[r]) for every place, q [m, h] and w [n, ho, h] int8 as
+    topk_quantise_rows gives them, w_scale [n, ho], r as in topk_expert_product_fwd.  Rows behind offset[n] are not written."""
+    n, ho, h, strides, (slots, off, src) = _eight(q, q_scale, w, w_scale, None, None, offset, source, dtype)
+    if out is not None:
+        _exact(out, (slots, ho), dtype, q, "out")
+        _apart((("out", out),), (q, q_scale, w, w_scale, offset, source))
+
+    def call(st):
+        y = _new(out, (slots, ho), dtype, q)
+        _check((_lib or load()).topk_expert_product_i8_fwd(
+            q.data_ptr(), q.stride(0), q.shape[0], q_scale.data_ptr(), w.data_ptr(), strides[0], strides[1], w_scale.data_ptr(),
+            off, src, int(k), slots, n, h, ho, _TYPES[dtype], y.data_ptr(), st), "topk_expert_product_i8_fwd")
+        return y
+    return _on(q, stream, call)
+
+
+def topk_expert_gated_i8_fwd(q, q_scale, w_gate, gate_scale, w_up, up_scale, offset, source=None, k=1, act=TOPK_ACT_SILU,
+                             dtype=torch.bfloat16, out=None, stream=None):
+    """Returns out [slots, f] of dtype: act(g) * u for every place, g and u the products of topk_expert_product_i8_fwd with the two
+    weights [n, f, h].  Rows behind offset[n] are not written."""
+    n, f, h, strides, (slots, off, src) = _eight(q, q_scale, w_gate, gate_scale, w_up, up_scale, offset, source, dtype)
+    if out is not None:
+        _exact(out, (slots, f), dtype, q, "out")
+        _apart((("out", out),), (q, q_scale, w_gate, gate_scale, w_up, up_scale, offset, source))
+
+    def call(st):
+        y = _new(out, (slots, f), dtype, q)
+        _check((_lib or load()).topk_expert_gated_i8_fwd(
+            q.data_ptr(), q.stride(0), q.shape[0], q_scale.data_ptr(), w_gate.data_ptr(), gate_scale.data_ptr(), w_up.data_ptr(),
+            up_scale.data_ptr(), strides[0], strides[1], off, src, int(k), slots, n, h, f, _TYPES[dtype], int(act), y.data_ptr(),
+            st), "topk_expert_gated_i8_fwd")
+        return y
+    return _on(q, stream, call)

@@ -27,6 +27,12 @@ template <>
 struct FragmentOf<float> {
   using type = f32x4;
 };
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
+template <>
+struct FragmentOf<int8_t> {
+  using type = i32x4;
+};
 // 16 bytes of k of one row
 template <class T>
 using Fragment = typename FragmentOf<T>::type;
@@ -46,6 +52,9 @@ __device__ __forceinline__ f32x16 mma(int, f16x8 a, f16x8 b, f32x16 c) {
 }
 __device__ __forceinline__ f32x16 mma(int q, f32x4 a, f32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x2f32(a[q], b[q], c, 0, 0, 0);
+}
+__device__ __forceinline__ i32x16 mma(int, i32x4 a, i32x4 b, i32x16 c) {
+  return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0);
 }
 
 // x / d for 0 <= x < 2^31: with s = ceil(log2 d) and M = floor(2^(31 + s) / d) + 1, M d = 2^(31 + s) + e with 0 < e <= 2^s, so

@@ -18,48 +18,12 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// a tile of ROWS x COLS (A, B), steps of STEP bytes of k, 2 x 2 wavefronts
-template <class T_, int ROWS, int COLS, int STEP>
-struct Tile {
-  using T = T_;
-  static constexpr int kRows = ROWS, kCols = COLS, kStep = STEP;
-  static constexpr int kStageBytes = (ROWS + COLS) * STEP;
-  static constexpr int MI = ROWS / 2 / 32, NJ = COLS / 2 / 32;
-  template <bool KC>
-  using A = Image<T, KC, ROWS, kThreads, STEP>;
-  template <bool KC>
-  using B = Image<T, KC, COLS, kThreads, STEP>;
-  using Sums = f32x16[MI][NJ];
-  static __device__ __forceinline__ int wave_row() { return (int(threadIdx.x) / kWave & 1) * (ROWS / 2); }
-  static __device__ __forceinline__ int wave_col() { return (int(threadIdx.x) / kWave >> 1) * (COLS / 2); }
-};
 template <class T>
 using Wide = Tile<T, 128, 256, 64>;
 template <class T, int STEP>
 using Middle = Tile<T, 128, 128, STEP>;
 template <class T>
 using Small = Tile<T, 64, 64, 128>;
-
-// between(turn, turns): what is done between the matrix instructions
-template <class TILE, class IA, class IB, class F>
-__device__ __forceinline__ void multiply(const char* stage, typename TILE::Sums& acc, F between) {
-#pragma unroll
-  for (int t = 0; t < TILE::kStep / 32; ++t) {
-    Fragment<typename TILE::T> fa[TILE::MI], fb[TILE::NJ];
-#pragma unroll
-    for (int i = 0; i < TILE::MI; ++i) fa[i] = IA::read(stage, TILE::wave_row() + 32 * i, t);
-#pragma unroll
-    for (int j = 0; j < TILE::NJ; ++j) fb[j] = IB::read(stage + IA::kBytes, TILE::wave_col() + 32 * j, t);
-#pragma unroll
-    for (int q = 0; q < kMma<typename TILE::T>; ++q)
-#pragma unroll
-      for (int j = 0; j < TILE::NJ; ++j) {
-#pragma unroll
-        for (int i = 0; i < TILE::MI; ++i) acc[i][j] = mma(q, fb[j], fa[i], acc[i][j]);
-        between((t * kMma<typename TILE::T> + q) * TILE::NJ + j, TILE::kStep / 32 * kMma<typename TILE::T> * TILE::NJ);
-      }
-  }
-}
 
 // Sums over `depth` k.  LISTED: rows of k are looked up in `table`, which is filled on the way.
 template <class TILE, class IA, class IB, bool LISTED, class LA, class LB>
@@ -143,12 +107,6 @@ __device__ __forceinline__ void sum_staged(char* lds, LA& a, LB& b, const Table&
     if (kApart && (k0 & (2 * IA::kStepK)) != 0) add_part();
   }
   if constexpr (kApart) add_part();
-}
-
-// First column (row) of tile number `tile` of `end`, `size` each.  The last one ends where the operand ends, and computes again,
-// alike, what it shares with the one before: no part of it crosses the end.
-__device__ __forceinline__ int64_t tile_start(int64_t tile, int64_t size, int64_t end) {
-  return min(tile * size, max(end - size, int64_t(0)));
 }
 
 template <class TILE, bool B_KC, bool TINY>

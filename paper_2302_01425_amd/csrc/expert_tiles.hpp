@@ -16,7 +16,9 @@ __device__ const uint4 zero_part = {0, 0, 0, 0};     // read in the place of wha
 // and gets 4 k of one column per lane); half a wavefront reads 64 bytes of four rows, so blocks of 64 bytes change places by
 // k % 4 (rows of 128 bytes: by k / 2 % 2, odd and even ones lie in different banks anyway).  float32 is read element by
 // element, 128 bytes of two rows that are four apart; blocks of 128 bytes change places by k / 4 % 2.
-template <class T, bool KC, int R, int THREADS, int STEP>
+// PAIR: of the R rows, 32 of a first operand and 32 of a second one of the same numbers come in turn, so that a wavefront that
+// has two such blocks holds what both operands make of the same columns in the same lanes and registers.
+template <class T, bool KC, int R, int THREADS, int STEP, bool PAIR = false>
 struct Image {
   using Type = T;
   static constexpr bool kKC = KC;
@@ -26,7 +28,12 @@ struct Image {
   static constexpr int kParts = kBytes / 16 / THREADS;   // per thread
   static constexpr int kStepK = STEP / int(sizeof(T));
   static constexpr int kAlong = KC ? STEP / 16 : R / N;  // parts of an image row
+  static constexpr int kSpan = PAIR ? R / 2 : R;         // rows of an operand
   static_assert(R >= 64 && (STEP == 64 || STEP == 128), "exchanges stay inside a row");
+
+  // row of the operand behind row r of the image, and whether it is the second operand's
+  static __device__ __forceinline__ int place(int r) { return PAIR ? (r >> 6 << 5) + (r & 31) : r; }
+  static __device__ __forceinline__ bool second(int r) { return PAIR && (r & 32) != 0; }
 
   // what the number of a part in image row r is changed by
   static __device__ __forceinline__ int exchange(int r) {
@@ -129,24 +136,27 @@ struct Direct {
 
   // Rows [first, end) of an operand contiguous in k, found through source where there is one.  Rows behind the last, and rows
   // whose place has none, are read from another row; their outputs are not stored, or stored as zeros.
+  // (`apart`: bytes from the first operand of a pair to the second, here and below)
   __device__ __forceinline__ void init_rows(const void* base, int64_t row_stride, const int32_t* source, const Divisor& d,
-                                            int64_t limit, int64_t first, int64_t end) {
+                                            int64_t limit, int64_t first, int64_t end, int64_t apart = 0) {
 #pragma unroll
     for (int i = 0; i < IMAGE::kParts; ++i) {
-      int64_t row = min(first + IMAGE::row_of(i), end - 1);
+      int64_t row = min(first + IMAGE::place(IMAGE::row_of(i)), end - 1);
       if (source != nullptr) row = min(int64_t(quotient(max(source[row], 0), d)), limit - 1);
       p[i] = static_cast<const char*>(base) + row * row_stride * int64_t(sizeof(T)) + IMAGE::part_of(i) * 16;
+      if (IMAGE::second(IMAGE::row_of(i))) p[i] += apart;
     }
   }
   // Columns [first, end) of an operand with one row per k, from row k_begin on; columns behind the last as above.
   __device__ __forceinline__ void init_columns(const void* base, int64_t row_stride, const int32_t* rows, int64_t first,
-                                               int64_t end, int64_t k_begin) {
+                                               int64_t end, int64_t k_begin, int64_t apart = 0) {
     stride = row_stride * int64_t(sizeof(T));
     table = rows;
 #pragma unroll
     for (int i = 0; i < IMAGE::kParts; ++i) {
-      const int64_t at = min(first + IMAGE::part_of(i) * IMAGE::N, end - IMAGE::N);
+      const int64_t at = min(first + IMAGE::place(IMAGE::part_of(i) * IMAGE::N), end - IMAGE::N);
       p[i] = static_cast<const char*>(base) + at * int64_t(sizeof(T));
+      if (IMAGE::second(IMAGE::part_of(i) * IMAGE::N)) p[i] += apart;
       if (ORDER != kListed) p[i] += (k_begin + IMAGE::row_of(i)) * stride;
     }
   }
@@ -154,7 +164,9 @@ struct Direct {
   // part i of the step k0 .. to LDS at `to` (of the step's image), zeros from `depth` on; without branches.  `there`: the table's
   // bits of the step, read once (both gradients of 8192 tokens x 2, 32 experts, 2048 -> 4096: 745 us, 748 with a look into the
   // table for every part, 739 without either; with code of its own for steps that have such a place the sums left the registers)
-  __device__ __forceinline__ void issue_part(int i, int64_t k0, int64_t depth, uint32_t to, uint32_t there = 0) const {
+  // `ahead` (kInOrder): bytes that are added to every address, as for the second of two sums over the same k.
+  __device__ __forceinline__ void issue_part(int i, int64_t k0, int64_t depth, uint32_t to, uint32_t there = 0,
+                                             int64_t ahead = 0) const {
     const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
     const char* zeros = reinterpret_cast<const char*>(&zero_part);
     const char* from;
@@ -166,7 +178,7 @@ struct Direct {
       static_assert(IMAGE::kStepK == 32, "a word per step");
       from = (there >> IMAGE::row_of(i) & 1u) != 0 ? p[i] + k0 * stride : zeros;
     } else {
-      from = p[i] + k0 * (KC ? int64_t(sizeof(T)) : stride);
+      from = p[i] + (k0 * (KC ? int64_t(sizeof(T)) : stride) + ahead);
       const int left = int(min(depth - k0, int64_t(IMAGE::kStepK)));
       from = (KC ? IMAGE::part_of(i) * IMAGE::N : IMAGE::row_of(i)) < left ? from : zeros;
     }
@@ -190,35 +202,41 @@ struct Staged {
   Fragment<T> v[2][IMAGE::kParts];
 
   __device__ __forceinline__ void init_rows(const void* base, int64_t row_stride, const int32_t* source, const Divisor& d,
-                                            int64_t limit, int64_t first, int64_t end) {
+                                            int64_t limit, int64_t first, int64_t end, int64_t apart = 0) {
 #pragma unroll
     for (int i = 0; i < IMAGE::kParts; ++i) {
-      int64_t row = min(first + IMAGE::row_of(i), end - 1);
+      int64_t row = min(first + IMAGE::place(IMAGE::row_of(i)), end - 1);
       bool there = true;
       if (source != nullptr) {
         const int pair = source[row];
         row = quotient(max(pair, 0), d);
         there = pair >= 0 && row < limit;
       }
-      p[i] = there ? static_cast<const T*>(base) + row * row_stride + IMAGE::part_of(i) * N : nullptr;
+      const char* from = static_cast<const char*>(base);
+      if (IMAGE::second(IMAGE::row_of(i))) from += apart;
+      p[i] = there ? reinterpret_cast<const T*>(from) + row * row_stride + IMAGE::part_of(i) * N : nullptr;
     }
   }
   __device__ __forceinline__ void init_columns(const void* base, int64_t row_stride, const int32_t* rows, int64_t first,
-                                               int64_t end, int64_t k_begin) {
+                                               int64_t end, int64_t k_begin, int64_t apart = 0) {
     stride = row_stride;
     table = rows;
     edge = end - first;
 #pragma unroll
     for (int i = 0; i < IMAGE::kParts; ++i) {
       // (columns behind the end are not stored)
-      p[i] = static_cast<const T*>(base) + first + (TINY ? IMAGE::part_of(i) * N : min(int64_t(IMAGE::part_of(i) * N), edge - N));
+      const char* from = static_cast<const char*>(base);
+      if (IMAGE::second(IMAGE::part_of(i) * N)) from += apart;
+      p[i] = reinterpret_cast<const T*>(from) + first + (TINY ? int64_t(column(i)) : min(int64_t(column(i)), edge - N));
       if (ORDER != kListed) p[i] += (k_begin + IMAGE::row_of(i)) * stride;
     }
   }
 
+  // not KC: first column of part i, from the tile's first on
+  static __device__ __forceinline__ int column(int i) { return IMAGE::place(IMAGE::part_of(i) * N); }
   // how far part i, read in step k0, lies before its place
   __device__ __forceinline__ int behind(int i, int64_t k0, int64_t depth) const {
-    const int64_t over = (KC ? k0 : int64_t(0)) + IMAGE::part_of(i) * N + N - (KC ? depth : edge);
+    const int64_t over = KC ? k0 + IMAGE::part_of(i) * N + N - depth : column(i) + N - edge;
     return int(min(max(over, int64_t(0)), int64_t(N)));
   }
   // elements d .. of q, zeros behind them
@@ -229,6 +247,8 @@ struct Staged {
     if (bytes & 8) w = u32x4{w[2], w[3], 0u, 0u};
     if (bytes & 4) w = u32x4{w[1], w[2], w[3], 0u};
     if (bytes & 2) w = u32x4{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
+    if constexpr (sizeof(T) == 1)
+      if (bytes & 1) w = u32x4{w[0] >> 8 | w[1] << 24, w[1] >> 8 | w[2] << 24, w[2] >> 8 | w[3] << 24, w[3] >> 8};
     return __builtin_bit_cast(Fragment<T>, w);
   }
   static __device__ __forceinline__ Fragment<T> whole(const T* from) {
@@ -236,8 +256,8 @@ struct Staged {
     return __builtin_bit_cast(Fragment<T>, q);
   }
 
-  // the step k0 .. to the registers `set`, zeros from `depth` on
-  __device__ __forceinline__ void load(int set, int64_t k0, int64_t depth) {
+  // the step k0 .. to the registers `set`, zeros from `depth` on.  `ahead` as in Direct, in elements.
+  __device__ __forceinline__ void load(int set, int64_t k0, int64_t depth, int64_t ahead = 0) {
     const T* zeros = reinterpret_cast<const T*>(&zero_part);
 #pragma unroll
     for (int i = 0; i < IMAGE::kParts; ++i) {
@@ -245,7 +265,7 @@ struct Staged {
       bool there;
       if constexpr (KC) {
         there = p[i] != nullptr;
-        from = p[i] + k0;
+        from = p[i] + k0 + ahead;
       } else if constexpr (ORDER == kListed) {
         const int row = table[(int(k0) + IMAGE::row_of(i)) & (kTable - 1)];
         there = row >= 0;
@@ -253,12 +273,14 @@ struct Staged {
       } else {
         if constexpr (ORDER == kInOrderWhereListed) there = table[(int(k0) + IMAGE::row_of(i)) & (kTable - 1)] >= 0;
         else there = k0 + IMAGE::row_of(i) < depth;
-        from = p[i] + k0 * stride;
+        from = p[i] + k0 * stride + ahead;
       }
       if constexpr (TINY) {
-        const int64_t count = KC ? depth - (k0 + IMAGE::part_of(i) * N) : edge - IMAGE::part_of(i) * N;
+        const int64_t count = KC ? depth - (k0 + IMAGE::part_of(i) * N) : edge - column(i);
+        Packed<T, N> q;
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[set][i][j] = there && j < count ? from[j] : T(0.0f);
+        for (int j = 0; j < N; ++j) q.v[j] = there && j < count ? from[j] : T(0.0f);
+        v[set][i] = __builtin_bit_cast(Fragment<T>, q);
       } else {
         if constexpr (KC) {
           const int d = behind(i, k0, depth);
@@ -270,7 +292,7 @@ struct Staged {
     }
   }
   __device__ __forceinline__ void store(int set, char* to, int64_t k0, int64_t depth) const {
-    const bool cross = !TINY && (KC ? k0 + IMAGE::kStepK > depth : edge < IMAGE::kAlong * N);
+    const bool cross = !TINY && (KC ? k0 + IMAGE::kStepK > depth : edge < IMAGE::kSpan);
 #pragma unroll
     for (int i = 0; i < IMAGE::kParts; ++i) {
       Fragment<T> q = v[set][i];
@@ -292,10 +314,38 @@ __device__ __forceinline__ void store_columns(T* row, int64_t n, int64_t n_end, 
   }
 }
 
-// Sums of a wavefront to C: MI x NJ blocks of 32 x 32 from (m0, n0) on, below (m_end, n_end); n runs along the rows of the
+// 32 x 32 sums of a wavefront to a row of C per lane % 32, columns from n on, below n_end; n runs along the rows of the
 // instruction's output, so that a lane has four neighbouring columns at a time.  Of two such fours of 16-bit types, 8 columns
-// apart, lane l takes the first with that of lane l + 32 behind it, lane l + 32 the second: 16 bytes each.  Rows whose place has
-// no source are zeros.
+// apart, lane l takes the first with that of lane l + 32 behind it, lane l + 32 the second: 16 bytes each.  `inside`: the row is
+// one of C's; where `there` is false it is one of zeros.
+template <class T>
+__device__ __forceinline__ void store_block(const f32x16& acc, T* row, bool inside, bool there, int64_t n, int64_t n_end) {
+  const int lane = int(threadIdx.x) & (kWave - 1);
+  Packed<T, 4> four[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) four[q].v[r] = from_f32<T>(there ? acc[4 * q + r] : 0.0f);
+  if constexpr (sizeof(T) == 2) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int q = 0; q < 4; q += 2) {
+      const u32x2 a = __builtin_bit_cast(u32x2, four[q]), b = __builtin_bit_cast(u32x2, four[q + 1]);
+      const auto x = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false);
+      const auto y = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
+      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+      const u32x4 w = {x[0], y[0], x[1], y[1]};
+      if (inside) store_columns<T, 8>(row, n + 8 * (q + (lane >> 5)), n_end, __builtin_bit_cast(Packed<T, 8>, w));
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (inside) store_columns<T, 4>(row, n + 8 * q + 4 * (lane >> 5), n_end, four[q]);
+  }
+}
+
+// Sums of a wavefront to C: MI x NJ blocks of 32 x 32 from (m0, n0) on, below (m_end, n_end).  Rows whose place has no source are
+// zeros.
 template <class T, int MI, int NJ>
 __device__ __forceinline__ void store_tile(const f32x16 (&acc)[MI][NJ], int64_t m0, int64_t m_end, int64_t n0, int64_t n_end,
                                            const int32_t* source, const Divisor& div, int64_t limit, T* c, int64_t c_stride) {
@@ -307,30 +357,7 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[MI][NJ], int64_t 
     if (there && source != nullptr) there = source[m] >= 0 && quotient(source[m], div) < limit;
     T* row = c + m * c_stride;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      Packed<T, 4> four[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) four[q].v[r] = from_f32<T>(there ? acc[i][j][4 * q + r] : 0.0f);
-      const int64_t n = n0 + 32 * j;
-      if constexpr (sizeof(T) == 2) {
-        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-#pragma unroll
-        for (int q = 0; q < 4; q += 2) {
-          const u32x2 a = __builtin_bit_cast(u32x2, four[q]), b = __builtin_bit_cast(u32x2, four[q + 1]);
-          const auto x = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false);
-          const auto y = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
-          typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-          const u32x4 w = {x[0], y[0], x[1], y[1]};
-          if (m < m_end) store_columns<T, 8>(row, n + 8 * (q + (lane >> 5)), n_end, __builtin_bit_cast(Packed<T, 8>, w));
-        }
-      } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (m < m_end) store_columns<T, 4>(row, n + 8 * q + 4 * (lane >> 5), n_end, four[q]);
-      }
-    }
+    for (int j = 0; j < NJ; ++j) store_block<T>(acc[i][j], row, m < m_end, there, n0 + 32 * j, n_end);
   }
 }
 
@@ -343,14 +370,58 @@ __device__ __forceinline__ void store_zeros(T* c, int64_t count, int64_t part, i
   if (part == 0 && threadIdx.x < count - whole * N) c[whole * N + threadIdx.x] = T(0.0f);
 }
 
-template <int MI, int NJ>
-__device__ __forceinline__ void clear(f32x16 (&acc)[MI][NJ]) {
+template <class ACC, int MI, int NJ>
+__device__ __forceinline__ void clear(ACC (&acc)[MI][NJ]) {
 #pragma unroll
   for (int i = 0; i < MI; ++i)
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+}
+
+// a tile of ROWS x COLS (A, B) of a workgroup of four wavefronts, 2 x 2, steps of STEP bytes of k
+template <class T_, int ROWS, int COLS, int STEP, bool PAIR = false>
+struct Tile {
+  using T = T_;
+  static constexpr int kThreads = 4 * kWave;
+  static constexpr int kRows = ROWS, kCols = COLS, kStep = STEP;
+  static constexpr int kStageBytes = (ROWS + COLS) * STEP;
+  static constexpr int MI = ROWS / 2 / 32, NJ = COLS / 2 / 32;
+  template <bool KC>
+  using A = Image<T, KC, ROWS, kThreads, STEP>;
+  template <bool KC>
+  using B = Image<T, KC, COLS, kThreads, STEP, PAIR>;
+  using Sums = std::conditional_t<sizeof(T) == 1, i32x16, f32x16>[MI][NJ];
+  static __device__ __forceinline__ int wave_row() { return (int(threadIdx.x) / kWave & 1) * (ROWS / 2); }
+  static __device__ __forceinline__ int wave_col() { return (int(threadIdx.x) / kWave >> 1) * (COLS / 2); }
+};
+
+// between(turn, turns): what is done between the matrix instructions
+template <class TILE, class IA, class IB, class F>
+__device__ __forceinline__ void multiply(const char* stage, typename TILE::Sums& acc, F between) {
+#pragma unroll
+  for (int t = 0; t < TILE::kStep / 32; ++t) {
+    Fragment<typename TILE::T> fa[TILE::MI], fb[TILE::NJ];
+#pragma unroll
+    for (int i = 0; i < TILE::MI; ++i) fa[i] = IA::read(stage, TILE::wave_row() + 32 * i, t);
+#pragma unroll
+    for (int j = 0; j < TILE::NJ; ++j) fb[j] = IB::read(stage + IA::kBytes, TILE::wave_col() + 32 * j, t);
+#pragma unroll
+    for (int q = 0; q < kMma<typename TILE::T>; ++q)
+#pragma unroll
+      for (int j = 0; j < TILE::NJ; ++j) {
+#pragma unroll
+        for (int i = 0; i < TILE::MI; ++i) acc[i][j] = mma(q, fb[j], fa[i], acc[i][j]);
+        between((t * kMma<typename TILE::T> + q) * TILE::NJ + j, TILE::kStep / 32 * kMma<typename TILE::T> * TILE::NJ);
+      }
+  }
+}
+
+// First column (row) of tile number `tile` of `end`, `size` each.  The last one ends where the operand ends, and computes again,
+// alike, what it shares with the one before: no part of it crosses the end.
+__device__ __forceinline__ int64_t tile_start(int64_t tile, int64_t size, int64_t end) {
+  return min(tile * size, max(end - size, int64_t(0)));
 }
 
 }  // namespace topk

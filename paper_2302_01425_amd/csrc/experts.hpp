@@ -127,7 +127,7 @@ struct Packed {
   T v[N];
 };
 template <class T, int N>
-struct __attribute__((packed, aligned(2))) Loose {
+struct __attribute__((packed, aligned(sizeof(T) < 2 ? 1 : 2))) Loose {
   typename BitsOf<N * int(sizeof(T))>::type bits;
 };
 template <class T, int N>

@@ -1,0 +1,236 @@
+// What the kernels of the experts' feed-forward share: the gated block (two projections of the same rows, the activation and the
+// product), its gradients, and products in 8-bit integers.  Ragged rows, lists, tiles and operands as in expert_product.hpp.
+#pragma once
+
+#include "expert_tiles.hpp"
+
+namespace topk {
+
+enum ActCode : int { kSilu = 0, kGelu = 1, kGeluTanh = 2, kRelu = 3 };
+
+// What becomes of the sums of a tile:
+//   kPlain   8-bit operands: c = a_scale w_scale sum
+//   kOut     of a pair of weights, g and u: c = act(g) u, and the sums themselves to `pre`
+//   kSlopes  of a pair, with the cotangent t of act(g) u: t u act'(g) and t act(g), side by side in a row of c
+//   kBoth    rows of such slopes times the pair, c = dg W + du W'
+enum Work { kPlain, kOut, kSlopes, kBoth };
+constexpr bool is_pair(Work w) { return w == kOut || w == kSlopes; }
+
+struct FeedArgs : RowsArgs {
+  int64_t apart;            // bytes from w to the second weights
+  int64_t a_apart;          // kBoth: bytes from a's dg to its du
+  int64_t c_stride;         // elements between rows of c; kSlopes: two halves
+  int act, out_type;
+  void* pre;                // kOut: [slots][2][cols] or null
+  const void* t;            // kSlopes
+  int64_t t_stride;
+  const float *a_scale;     // 8-bit: of the rows of a
+  const float *w_scale, *u_scale;      // [n][cols]
+};
+
+// ---- activations --------------------------------------------------------------------------------------------------------
+// exp(x): for outputs of 16 bits by the hardware's exp2, off by |x| 2^-24 and two steps more
+template <bool FINE>
+__device__ __forceinline__ float exp_of(float x) {
+  if constexpr (FINE) return expf(x);
+  else return __builtin_amdgcn_exp2f(x * 1.44269504f);
+}
+template <bool FINE>
+__device__ __forceinline__ float inverse(float x) {
+  if constexpr (FINE) return 1.0f / x;
+  else return __builtin_amdgcn_rcpf(x);
+}
+
+// act(g) and act'(g).  Each comes from a form that keeps its digits where g is far below zero:
+//   silu       g p, p = 1 / (1 + exp(-g));  p + g p (1 - p)
+//   gelu       g F, F = P(N(0, 1) < g);  F + g exp(-g^2 / 2) / sqrt(2 pi).  F(-|g|) = exp(-g^2 / 2) q(t) t, t = 1 / (1 + 0.4 |g| /
+//              sqrt 2), with q the polynomial of degree 10 through the Chebyshev nodes of t in (0, 1) of exp(x^2) erfc(x) / 2 t, x =
+//              (1 / t - 1) / 0.4: off by 8e-9 of it, 3.2e-7 in float32.  g^2 is taken with the rounding it lost.
+//   gelu_tanh  g (1 + tanh z) / 2 = g p(2 z), z = sqrt(2 / pi) (g + 0.044715 g^3)
+//   relu       g where g > 0, slope 0 at 0
+template <int ACT, bool FINE>
+__device__ __forceinline__ float act_value(float g, float* slope) {
+  if constexpr (ACT == kSilu) {
+    const float p = inverse<FINE>(1.0f + exp_of<FINE>(-g));
+    if (slope != nullptr) *slope = p + g * p * (1.0f - p);
+    return g * p;
+  } else if constexpr (ACT == kGelu) {
+    const float s = g * g;
+    const float e = s < 208.0f ? exp_of<FINE>(-0.5f * s) * (1.0f - 0.5f * __builtin_fmaf(g, g, -s)) : 0.0f;
+    const float t = inverse<FINE>(1.0f + 0.282842712f * fabsf(g));
+    constexpr float kQ[11] = {0.112837916f, 0.112838158f, 0.10380036f, 0.085945286f, 0.0590475614f, 0.0435603211f,
+                              -0.0268965838f, 0.0734016237f, -0.121520867f, 0.071920535f, -0.0149343143f};
+    float q = kQ[10];
+#pragma unroll
+    for (int i = 9; i >= 0; --i) q = __builtin_fmaf(q, t, kQ[i]);
+    const float tail = e * t * q;
+    const float p = g < 0.0f ? tail : 1.0f - tail;
+    if (slope != nullptr) *slope = __builtin_fmaf(g * e, 0.398942280f, p);
+    return g * p;
+  } else if constexpr (ACT == kGeluTanh) {
+    const float b = fminf(fmaxf(g, -30.0f), 30.0f), b2 = b * b;      // (beyond, p is 0 or 1)
+    const float z2 = 1.59576912f * b * __builtin_fmaf(0.044715f, b2, 1.0f);
+    const float p = inverse<FINE>(1.0f + exp_of<FINE>(-z2));
+    if (slope != nullptr) *slope = p + b * p * (1.0f - p) * 1.59576912f * __builtin_fmaf(0.134145f, b2, 1.0f);
+    return g * p;
+  } else {
+    if (slope != nullptr) *slope = g > 0.0f ? 1.0f : 0.0f;
+    return g > 0.0f ? g : 0.0f;
+  }
+}
+
+// ---- outputs --------------------------------------------------------------------------------------------------------------
+template <class T>
+__device__ __forceinline__ void load_four(const T* p, int64_t left, float (&v)[4]) {
+  if (left >= 4) {
+    const Packed<T, 4> q = load_packed<T, 4>(p);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = to_f32(q.v[r]);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = r < left ? to_f32(p[r]) : 0.0f;
+  }
+}
+
+// Sums of a wavefront, MI x NJ blocks of 32 x 32 from row m0 on (below m_end), to the outputs from column n0 on.  Rows whose place
+// has no source are zeros, whatever their operands hold.  T: type of the operands; OUT: of c.
+template <class T, class OUT, Work WORK, int ACT, int MI, int NJ, class ACC>
+__device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const FeedArgs& g, int expert, int64_t m0, int64_t m_end,
+                                            int64_t n0) {
+  constexpr bool kEight = sizeof(T) == 1, kFine = sizeof(OUT) == 4;
+  constexpr int kOf = is_pair(WORK) ? 2 : 1;
+  const int lane = int(threadIdx.x) & (kWave - 1);
+  bool there[MI];
+  float scale[MI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int64_t m = m0 + 32 * i + (lane & 31);
+    int64_t row = m;
+    there[i] = m < m_end;
+    if (there[i] && g.source != nullptr) {
+      const int pair = g.source[m];
+      row = quotient(max(pair, 0), g.div);
+      there[i] = pair >= 0 && row < g.limit;
+    }
+    scale[i] = kEight && there[i] ? g.a_scale[row] : 0.0f;
+  }
+#pragma unroll
+  for (int j = 0; j < NJ; j += kOf) {
+    const int64_t n = n0 + 32 * (j / kOf), mine = n + 4 * (lane >> 5);
+    float ws[4][4], us[4][4];
+    if constexpr (kEight) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        load_four(g.w_scale + expert * g.cols + mine + 8 * q, g.cols - mine - 8 * q, ws[q]);
+        if constexpr (kOf == 2) load_four(g.u_scale + expert * g.cols + mine + 8 * q, g.cols - mine - 8 * q, us[q]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int64_t m = m0 + 32 * i + (lane & 31);
+      const bool inside = m < m_end;
+      OUT* row = static_cast<OUT*>(g.c) + m * g.c_stride;
+      f32x16 first, second;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int x = 4 * q + r;
+          first[x] = kEight ? float(acc[i][j][x]) * scale[i] * ws[q][r] : float(acc[i][j][x]);
+          if constexpr (kOf == 2) second[x] = kEight ? float(acc[i][j + 1][x]) * scale[i] * us[q][r] : float(acc[i][j + 1][x]);
+        }
+      }
+      if constexpr (kOf == 1) {
+        store_block<OUT>(first, row, inside, there[i], n, g.cols);
+      } else if constexpr (WORK == kOut) {
+        if constexpr (!kEight) {
+          if (g.pre != nullptr) {
+            T* sums = static_cast<T*>(g.pre) + m * 2 * g.cols;
+            store_block<T>(first, sums, inside, there[i], n, g.cols);
+            store_block<T>(second, sums + g.cols, inside, there[i], n, g.cols);
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < 16; ++x) first[x] = act_value<ACT, kFine>(first[x], nullptr) * second[x];
+        store_block<OUT>(first, row, inside, there[i], n, g.cols);
+      } else {
+        const T* t = static_cast<const T*>(g.t) + m * g.t_stride;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float tv[4];
+          load_four(t + mine + 8 * q, there[i] ? g.cols - mine - 8 * q : int64_t(0), tv);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int x = 4 * q + r;
+            float slope;
+            const float value = act_value<ACT, kFine>(first[x], &slope);
+            first[x] = tv[r] * second[x] * slope;
+            second[x] = tv[r] * value;
+          }
+        }
+        // (rounded to the operands' type, which the matrix instructions of the gradients take)
+        store_block<OUT>(first, row, inside, there[i], n, g.cols);
+        store_block<OUT>(second, row + g.c_stride / 2, inside, there[i], n, g.cols);
+      }
+    }
+  }
+}
+
+template <class T, class OUT, Work WORK, int MI, int NJ, class ACC>
+__device__ __forceinline__ void finish_act(const ACC (&acc)[MI][NJ], const FeedArgs& g, int expert, int64_t m0, int64_t m_end,
+                                           int64_t n0) {
+  if constexpr (!is_pair(WORK)) {
+    finish_tile<T, OUT, WORK, 0>(acc, g, expert, m0, m_end, n0);
+  } else {
+    if (g.act == kSilu) finish_tile<T, OUT, WORK, kSilu>(acc, g, expert, m0, m_end, n0);
+    else if (g.act == kGelu) finish_tile<T, OUT, WORK, kGelu>(acc, g, expert, m0, m_end, n0);
+    else if (g.act == kGeluTanh) finish_tile<T, OUT, WORK, kGeluTanh>(acc, g, expert, m0, m_end, n0);
+    else finish_tile<T, OUT, WORK, kRelu>(acc, g, expert, m0, m_end, n0);
+  }
+}
+
+// ---- launchers: which kernel takes a call is decided in feed_forward.hip -----------------------------------------------------
+// tiles of feed_tiles.hpp: rows of any alignment.  float32 takes kSmall
+template <class T>
+int launch_feed_tiles(const FeedArgs& g, bool k_contiguous, Work work, TileKind kind, hipStream_t stream);
+
+// elementwise: slopes from the sums that the forward pass kept
+int launch_slopes(int type, const FeedArgs& g, hipStream_t stream);
+
+struct GatedArgs {
+  ProductArgs p;             // w: gate, ho: f; out, dx; dw: gate
+  const void* w_up;
+  void *pre, *dw_up;
+  const void* kept;          // pre of the forward pass or null
+  int act;
+  void* scratch;
+};
+int64_t slopes_stride(int type, int64_t f);      // elements between rows of slopes
+int launch_gated_fwd(int type, const GatedArgs& g, hipStream_t stream);
+int launch_gated_vjp(int type, const GatedArgs& g, hipStream_t stream);
+
+struct EightArgs {
+  const int8_t* x;
+  int64_t x_stride, m;
+  const float* x_scale;
+  const int8_t *w, *w_up;    // w_up null: the plain product
+  int64_t w_expert, w_out;
+  const float *w_scale, *up_scale;
+  const int32_t *offset, *source;
+  int64_t k, slots;
+  int n;
+  int64_t h, f;
+  int act, out_type;
+  void* out;
+};
+int launch_eight(const EightArgs& g, hipStream_t stream);
+
+struct QuantiseArgs {
+  const void* x;
+  int64_t x_stride, m, h;
+  int8_t* q;
+  float* scale;
+};
+int launch_quantise(int type, const QuantiseArgs& g, hipStream_t stream);
+
+}  // namespace topk
