@@ -121,10 +121,11 @@ _CALL_ENTRIES = ("topk_mask_fwd", "topk_mask_jvp", "topk_mask_vjp", "topkmag_fwd
                  "topk_signed_mask_fwd", "topk_signed_mask_jvp", "topk_masked_value_fwd", "topk_masked_value_jvp",
                  "topk_mask_sparse_fwd", "topk_mask_loss", "topk_route_fwd", "topk_route_vjp", "topk_expert_map",
                  "topk_expert_map_bytes", "topk_expert_product_fwd", "topk_expert_product_vjp", "topk_combine_fwd",
-                 "topk_combine_vjp")
+                 "topk_combine_vjp", "topk_expert_gated_fwd", "topk_expert_gated_vjp", "topk_expert_gated_vjp_bytes",
+                 "topk_quantise_rows", "topk_expert_product_i8_fwd", "topk_expert_gated_i8_fwd")
 (_MASK_FWD, _MASK_JVP, _MASK_VJP, _MAG_FWD, _MAG_JVP, _MAG_VJP, _SIGNED_FWD, _SIGNED_JVP, _MASKED_FWD, _MASKED_JVP,
  _SPARSE, _LOSS, _ROUTE_FWD, _ROUTE_VJP, _MAP, _MAP_BYTES, _PRODUCT_FWD, _PRODUCT_VJP, _COMBINE_FWD,
- _COMBINE_VJP) = range(len(_CALL_ENTRIES))
+ _COMBINE_VJP, _GATED_FWD, _GATED_VJP, _GATED_BYTES, _QUANTISE, _PRODUCT_I8, _GATED_I8) = range(len(_CALL_ENTRIES))
 
 
 def _load_call(L: ctypes.CDLL) -> None:
@@ -929,6 +930,10 @@ def topk_expert_gated_fwd(x, w_gate, w_up, offset, source=None, k=1, act=TOPK_AC
     """Returns out [slots, f]: act(W_gate[e] x[r]) * (W_up[e] x[r]) for every place, r as in topk_expert_product_fwd, both weights
     [n, f, h]; with want_pre (or pre_out) (out, pre), pre [slots, 2, f] both sums for topk_expert_gated_vjp.  Rows behind
     offset[n] are not written."""
+    if _call is not None and out is None and pre_out is None:
+        r = _call.gated_fwd(_GATED_FWD, x, w_gate, w_up, offset, source, k, act, want_pre, stream)
+        if r is not None:
+            return r
     x, slots, n, f, h, _, args = _gated(x, w_gate, w_up, offset, source, k, act)
     for t, shape, name in ((out, (slots, f), "out"), (pre_out, (slots, 2, f), "pre_out")):
         if t is not None:
@@ -950,6 +955,10 @@ def topk_expert_gated_vjp(x, w_gate, w_up, offset, cotangent, source=None, k=1, 
     """Returns (dx [slots, h] per place, dw_gate, dw_up like the weights); what is not wanted is None.  pre: what the forward pass
     returned with want_pre; without it both projections are computed again.  Rows of dx behind offset[n] are not written; with
     source, topk_combine_fwd(dx, slot) gives the gradient of x."""
+    if _call is not None and dx_out is None and dw_gate_out is None and dw_up_out is None:
+        r = _call.gated_vjp(_GATED_VJP, _GATED_BYTES, x, w_gate, w_up, offset, source, k, act, cotangent, pre, want_x, want_w, stream)
+        if r is not None:
+            return r
     x, slots, n, f, h, plain, args = _gated(x, w_gate, w_up, offset, source, k, act)
     cotangent = _rows(cotangent, "cotangent", x)
     if tuple(cotangent.shape) != (slots, f):
@@ -986,6 +995,10 @@ def topk_expert_gated_vjp(x, w_gate, w_up, offset, cotangent, source=None, k=1, 
 
 def topk_quantise_rows(x, q_out=None, scale_out=None, stream=None):
     """Returns (q [m, h] int8, scale [m] float32) with x about q * scale per row: tokens, or weights seen as [n * out, in]."""
+    if _call is not None and q_out is None and scale_out is None:
+        r = _call.quantise(_QUANTISE, x, stream)
+        if r is not None:
+            return r
     x = _rows(x, "x")
     m, h = x.shape
     for t, shape, dtype, name in ((q_out, (m, h), torch.int8, "q_out"), (scale_out, (m,), _F32, "scale_out")):
@@ -1025,6 +1038,10 @@ def _eight(q, q_scale, w, w_scale, w_up, up_scale, offset, source, dtype):
 def topk_expert_product_i8_fwd(q, q_scale, w, w_scale, offset, source=None, k=1, dtype=torch.bfloat16, out=None, stream=None):
     """Returns out [slots, ho] of dtype: q_scale[r] * w_scale[e] * (W[e] q[r]) for every place, q [m, h] and w [n, ho, h] int8 as
     topk_quantise_rows gives them, w_scale [n, ho], r as in topk_expert_product_fwd.  Rows behind offset[n] are not written."""
+    if _call is not None and out is None and dtype in _TYPES:
+        r = _call.eight(_PRODUCT_I8, q, q_scale, w, w_scale, None, None, offset, source, k, 0, _TYPES[dtype], stream)
+        if r is not None:
+            return r
     n, ho, h, strides, (slots, off, src) = _eight(q, q_scale, w, w_scale, None, None, offset, source, dtype)
     if out is not None:
         _exact(out, (slots, ho), dtype, q, "out")
@@ -1043,6 +1060,10 @@ def topk_expert_gated_i8_fwd(q, q_scale, w_gate, gate_scale, w_up, up_scale, off
                              dtype=torch.bfloat16, out=None, stream=None):
     """Returns out [slots, f] of dtype: act(g) * u for every place, g and u the products of topk_expert_product_i8_fwd with the two
     weights [n, f, h].  Rows behind offset[n] are not written."""
+    if _call is not None and out is None and dtype in _TYPES:
+        r = _call.eight(_GATED_I8, q, q_scale, w_gate, gate_scale, w_up, up_scale, offset, source, k, act, _TYPES[dtype], stream)
+        if r is not None:
+            return r
     n, f, h, strides, (slots, off, src) = _eight(q, q_scale, w_gate, gate_scale, w_up, up_scale, offset, source, dtype)
     if out is not None:
         _exact(out, (slots, f), dtype, q, "out")

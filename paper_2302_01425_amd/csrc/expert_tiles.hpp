@@ -128,6 +128,7 @@ enum Order { kInOrder, kListed, kInOrderWhereListed };
 // sum's first.
 template <class IMAGE, Order ORDER>
 struct Direct {
+  using Image = IMAGE;
   using T = typename IMAGE::Type;
   static constexpr bool KC = IMAGE::kKC;
   const char* p[IMAGE::kParts];    // the part at k = 0 (kListed: its column of row 0)

@@ -22,9 +22,56 @@ int64_t row_tiles(const FeedArgs& g, int64_t rows, int64_t cols) {
   return min(int64_t(g.n), g.slots) * cut(even_share(g.slots, g.n), rows) * cut(g.cols, cols);
 }
 
+// rows made of whole 16-byte parts that start at 16-byte boundaries
+bool whole_parts(const void* p, int64_t stride, int64_t length, int size) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0 && length * size % 16 == 0;
+}
+
+// Which kernel takes the rows (us, from a graph of calls with W from HBM; experts x places each, h -> f; gated bfloat16 where
+// nothing else is said):
+//   four rows at a time (few) / 32 rows of half the columns (narrow) / 32 rows (thin) / 64 rows (small): what bounds the first is
+//     multiplications, of the others loads in flight per compute unit, then operands read again.
+//     1 x 1 2048 -> 1024 6.0 / 9.4 / 13.9 / 25, 1 x 8 9.4 / 10.1 / 14.7 / 25, 1 x 32 20 / 12.2 / 16.9 / 25, 8 x 8 512 -> 512 7.4 / 6.0
+//     / 7.4 / 10.2, 8 x 16 2048 -> 1024 66 / 20.6 / 20.1 / 32, 8 x 64 211 / 38 / 31 / 33, 32 x 8 137 / 59 / 51 / 68, 32 x 64 836 / -
+//     / 104 / 69, 1 x 128 4096 -> 4096 299 / 70 / 54 / 57, 2 x 128 564 / 135 / 102 / 62.
+//     Rows of W that do not begin at 16 bytes, 1001 -> 300: 8 x 4 7.8 / 14.4 / 21 / 19, 8 x 32 20 / 17.4 / 24 / 18.4, 32 x 4 15.4 /
+//     33 / 36 / 23.
+//     float32: 1 x 1 2048 -> 1024 7.1 / 14.9 / 25 / 95, 1 x 32 22 / 21 / 29 / 95, 8 x 32 144 / 47 / 45 / 108, 32 x 32 549 / 164 / 141 /
+//     196, 8 x 128 444 / 136 / 116 / 110, 8 x 1 4096 -> 4096 192 / 239 / 233 / 348, 8 x 128 1001 -> 300 62 / 28 / 35 / 55.
+//     8 bits, plain: 1 x 8 2048 -> 1024 4.8 / 7.7 / 10.9 / 12.7, 1 x 64 10.2 / 9.3 / 12.7 / 12.1, 8 x 64 39 / 14.9 / 13.3 / 13.5, 32 x 8
+//     24 / 21 / 20 / 16.5, 8 x 8 512 -> 512 6.4 / 5.2 / 6.8 / 6.7; gated: 1 x 8 5.5 / 8.4 / 11.1 / 14.9, 8 x 32 40 / 15.8 / 13.0 / 16.7,
+//     32 x 8 46 / 40 / 35 / 26.
+//   whole parts, 256 x 256: as the products of expert_product.hip.
 template <class T>
 int launch_feed(const FeedArgs& g, bool k_contiguous, Work work, hipStream_t stream) {
-  const bool middle = even_share(g.slots, g.n) >= 128 && row_tiles(g, 128, is_pair(work) ? 64 : 128) >= 200;
+  const int64_t share = even_share(g.slots, g.n), experts = min(int64_t(g.n), g.slots);
+  constexpr int s = int(sizeof(T));
+  const bool pair = is_pair(work);
+  const int64_t most = (int64_t(1) << 31) - (1 << 10);     // workgroups
+  // (limit 0: there is no row that could be read in the place of one that is out of range)
+  if (k_contiguous && work != kBoth && g.limit > 0 && g.depth * s >= 16 && (g.slots / 4 + g.n) * cut(g.cols, 2) < most) {
+    const bool aligned = reinterpret_cast<uintptr_t>(g.w) % 16 == 0 && g.w_stride * s % 16 == 0 && g.w_expert * s % 16 == 0 &&
+                         (!pair || g.apart % 16 == 0);
+    const int64_t fours = experts * cut(share, 4) * cut(g.cols, pair ? 2 : 4), multiplied = fours * 16 * g.depth;
+    const int64_t tiles = experts * cut(share, 32) * cut(g.cols, pair ? 32 : 64);
+    const bool few = s == 1 ? fours <= 1536 && multiplied <= (1 << 26)
+                   : s == 2 ? multiplied <= (aligned ? 1 << 25 : 100000000)
+                            : multiplied <= 100000000 || share <= 4;
+    if (few) return launch_feed_few<T>(g, work, stream);
+    if (tiles < (s == 2 && !aligned ? 96 : 192) || (s == 4 && !aligned && tiles < 1024))
+      return launch_feed_thin<T>(g, work, true, stream);
+    const bool thin = s == 1 ? tiles < 300 : s == 2 ? tiles < 768 || (tiles <= 1024 && share <= 16)
+                                                    : tiles < 1024 || (tiles == 1024 && share <= 32);
+    if (aligned && thin) return launch_feed_thin<T>(g, work, false, stream);
+  }
+  if constexpr (s < 4) {
+    const bool whole = g.limit > 0 && whole_parts(g.a, g.a_stride, g.depth, s) &&
+                       whole_parts(g.w, g.w_stride, k_contiguous ? g.depth : g.cols, s) && g.w_expert * s % 16 == 0 &&
+                       g.apart % 16 == 0 && (g.slots / 256 + g.n) * cut(g.cols, pair ? 128 : 256) < most;
+    if (whole && share >= 96 && row_tiles(g, 256, pair ? 128 : 256) >= 96)
+      return launch_feed_large<T>(g, k_contiguous, work, stream);
+  }
+  const bool middle = share >= 128 && row_tiles(g, 128, pair ? 64 : 128) >= 200;
   return launch_feed_tiles<T>(g, k_contiguous, work, middle ? kMiddle : kSmall, stream);
 }
 int launch_type(int type, const FeedArgs& g, bool k_contiguous, Work work, hipStream_t stream) {

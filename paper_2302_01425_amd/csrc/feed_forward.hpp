@@ -28,6 +28,54 @@ struct FeedArgs : RowsArgs {
   const float *w_scale, *u_scale;      // [n][cols]
 };
 
+// ---- tiles ----------------------------------------------------------------------------------------------------------------
+// As find_tile, with the tiles of rows of an expert in groups of kGroup, which meet all columns before the next: of the 32 tiles
+// that a die works on at a time, 8 x 4 read 12 panels, 32 x 1 would read 33.  Every wavefront finds the tile by itself, 64 experts
+// at a time.  (A die that takes an eighth of every expert's columns instead has the same work as the others, whatever the
+// experts' shares, but reads all rows of x: 32 experts of 480 rows, 2048 -> 2048 x 2, 300 us against 245; of unequal shares, 512
+// rows on average, 328 against 318.)
+// Fewer than 2^31 workgroups, so that all numbers fit 32 bits.
+constexpr uint32_t kGroup = 8;
+template <int ROWS>
+__device__ __forceinline__ bool find_group_tile(const FeedArgs& g, Found* f) {
+  const int lane = int(threadIdx.x) & (kWave - 1);
+  const uint32_t cols = uint32_t(g.col_tiles);
+  const auto tiles_of = [&](int e, int64_t* begin, int64_t* end) {
+    *begin = *end = 0;
+    if (e < g.n) places(g.offset, e, g.slots, begin, end);
+    return uint32_t((*end - *begin + ROWS - 1) / ROWS);
+  };
+  int64_t begin, end;
+  uint32_t total = 0;
+  for (int e = lane; e < g.n; e += kWave) total += tiles_of(e, &begin, &end);
+  for (int off = kWave / 2; off > 0; off >>= 1) total += uint32_t(__shfl_xor(int(total), off, kWave));
+  // (as dealt())
+  const uint32_t block = g.first + blockIdx.x, run = min(max(total * cols / (8 * kDies), 1u), uint32_t(kRunMost));
+  const uint32_t turn = block / kDies / run, pair = (turn * kDies + block % kDies) * run + (block / kDies - turn * run);
+  uint32_t start = 0;
+  for (int first = 0; first < g.n; first += kWave) {
+    const uint32_t tiles = tiles_of(first + lane, &begin, &end);
+    uint32_t scan = tiles;
+    for (int off = 1; off < kWave; off <<= 1) {
+      const uint32_t v = uint32_t(__shfl_up(int(scan), off, kWave));
+      if (lane >= off) scan += v;
+    }
+    const uint32_t before = (start + scan - tiles) * cols;
+    const unsigned long long here = __ballot(pair >= before && pair - before < tiles * cols);
+    if (here != 0) {
+      const int from = __ffsll(here) - 1;
+      const auto of = [&](uint32_t v) { return uint32_t(__builtin_amdgcn_readlane(int(v), from)); };
+      const uint32_t in = pair - of(before), group = in / (kGroup * cols), rest = in - group * kGroup * cols;
+      const uint32_t high = min(of(tiles) - group * kGroup, kGroup), col = rest / high;
+      const int64_t row = int64_t(of(uint32_t(begin))) + int64_t(group * kGroup + rest - col * high) * ROWS;
+      *f = Found{first + from, row, min(row + ROWS, int64_t(of(uint32_t(end)))), int64_t(col)};
+      return true;
+    }
+    start += uint32_t(__builtin_amdgcn_readlane(int(scan), kWave - 1));
+  }
+  return false;
+}
+
 // ---- activations --------------------------------------------------------------------------------------------------------
 // exp(x): for outputs of 16 bits by the hardware's exp2, off by |x| 2^-24 and two steps more
 template <bool FINE>
@@ -93,10 +141,10 @@ __device__ __forceinline__ void load_four(const T* p, int64_t left, float (&v)[4
 }
 
 // Sums of a wavefront, MI x NJ blocks of 32 x 32 from row m0 on (below m_end), to the outputs from column n0 on.  Rows whose place
-// has no source are zeros, whatever their operands hold.  T: type of the operands; OUT: of c.
+// has no source are zeros, whatever their operands hold.  Columns from n_end on are left as they were.  T: type of the operands; OUT: of c.
 template <class T, class OUT, Work WORK, int ACT, int MI, int NJ, class ACC>
 __device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const FeedArgs& g, int expert, int64_t m0, int64_t m_end,
-                                            int64_t n0) {
+                                            int64_t n0, int64_t n_end) {
   constexpr bool kEight = sizeof(T) == 1, kFine = sizeof(OUT) == 4;
   constexpr int kOf = is_pair(WORK) ? 2 : 1;
   const int lane = int(threadIdx.x) & (kWave - 1);
@@ -127,6 +175,7 @@ __device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const Feed
     }
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
+      if (m0 + 32 * i >= m_end) break;
       const int64_t m = m0 + 32 * i + (lane & 31);
       const bool inside = m < m_end;
       OUT* row = static_cast<OUT*>(g.c) + m * g.c_stride;
@@ -141,18 +190,18 @@ __device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const Feed
         }
       }
       if constexpr (kOf == 1) {
-        store_block<OUT>(first, row, inside, there[i], n, g.cols);
+        store_block<OUT>(first, row, inside, there[i], n, n_end);
       } else if constexpr (WORK == kOut) {
         if constexpr (!kEight) {
           if (g.pre != nullptr) {
             T* sums = static_cast<T*>(g.pre) + m * 2 * g.cols;
-            store_block<T>(first, sums, inside, there[i], n, g.cols);
-            store_block<T>(second, sums + g.cols, inside, there[i], n, g.cols);
+            store_block<T>(first, sums, inside, there[i], n, n_end);
+            store_block<T>(second, sums + g.cols, inside, there[i], n, n_end);
           }
         }
 #pragma unroll
         for (int x = 0; x < 16; ++x) first[x] = act_value<ACT, kFine>(first[x], nullptr) * second[x];
-        store_block<OUT>(first, row, inside, there[i], n, g.cols);
+        store_block<OUT>(first, row, inside, there[i], n, n_end);
       } else {
         const T* t = static_cast<const T*>(g.t) + m * g.t_stride;
 #pragma unroll
@@ -169,8 +218,8 @@ __device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const Feed
           }
         }
         // (rounded to the operands' type, which the matrix instructions of the gradients take)
-        store_block<OUT>(first, row, inside, there[i], n, g.cols);
-        store_block<OUT>(second, row + g.c_stride / 2, inside, there[i], n, g.cols);
+        store_block<OUT>(first, row, inside, there[i], n, n_end);
+        store_block<OUT>(second, row + g.c_stride / 2, inside, there[i], n, n_end);
       }
     }
   }
@@ -178,14 +227,14 @@ __device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const Feed
 
 template <class T, class OUT, Work WORK, int MI, int NJ, class ACC>
 __device__ __forceinline__ void finish_act(const ACC (&acc)[MI][NJ], const FeedArgs& g, int expert, int64_t m0, int64_t m_end,
-                                           int64_t n0) {
+                                           int64_t n0, int64_t n_end) {
   if constexpr (!is_pair(WORK)) {
-    finish_tile<T, OUT, WORK, 0>(acc, g, expert, m0, m_end, n0);
+    finish_tile<T, OUT, WORK, 0>(acc, g, expert, m0, m_end, n0, n_end);
   } else {
-    if (g.act == kSilu) finish_tile<T, OUT, WORK, kSilu>(acc, g, expert, m0, m_end, n0);
-    else if (g.act == kGelu) finish_tile<T, OUT, WORK, kGelu>(acc, g, expert, m0, m_end, n0);
-    else if (g.act == kGeluTanh) finish_tile<T, OUT, WORK, kGeluTanh>(acc, g, expert, m0, m_end, n0);
-    else finish_tile<T, OUT, WORK, kRelu>(acc, g, expert, m0, m_end, n0);
+    if (g.act == kSilu) finish_tile<T, OUT, WORK, kSilu>(acc, g, expert, m0, m_end, n0, n_end);
+    else if (g.act == kGelu) finish_tile<T, OUT, WORK, kGelu>(acc, g, expert, m0, m_end, n0, n_end);
+    else if (g.act == kGeluTanh) finish_tile<T, OUT, WORK, kGeluTanh>(acc, g, expert, m0, m_end, n0, n_end);
+    else finish_tile<T, OUT, WORK, kRelu>(acc, g, expert, m0, m_end, n0, n_end);
   }
 }
 
@@ -193,6 +242,17 @@ __device__ __forceinline__ void finish_act(const ACC (&acc)[MI][NJ], const FeedA
 // tiles of feed_tiles.hpp: rows of any alignment.  float32 takes kSmall
 template <class T>
 int launch_feed_tiles(const FeedArgs& g, bool k_contiguous, Work work, TileKind kind, hipStream_t stream);
+// tiles of feed_large.hpp: whole, aligned 16-byte parts, limit > 0; not float32
+template <class T>
+int launch_feed_large(const FeedArgs& g, bool k_contiguous, Work work, hipStream_t stream);
+
+// feed_few.hip: few rows per expert, limit > 0, W contiguous in k, 16 bytes of it at least; not kBoth
+template <class T>
+int launch_feed_few(const FeedArgs& g, Work work, hipStream_t stream);
+
+// feed_thin.hpp: few tiles, `narrow` for half as many columns each; otherwise as feed_few.hip
+template <class T>
+int launch_feed_thin(const FeedArgs& g, Work work, bool narrow, hipStream_t stream);
 
 // elementwise: slopes from the sums that the forward pass kept
 int launch_slopes(int type, const FeedArgs& g, hipStream_t stream);

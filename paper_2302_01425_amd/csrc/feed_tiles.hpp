@@ -75,7 +75,7 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void feed_tiles_kernel(FeedArgs 
   constexpr int kSums = WORK == kBoth ? 2 : 1;
   sum_steps<TILE, IA, IB, kSums>(lds, a, b, g.depth, g.a_apart / int64_t(sizeof(T)), g.apart / int64_t(sizeof(T)), acc);
   finish_act<T, OUT, WORK>(acc, g, f.expert, f.begin + TILE::wave_row(), f.end,
-                           n0 + TILE::wave_col() / (is_pair(WORK) ? 2 : 1));
+                           n0 + TILE::wave_col() / (is_pair(WORK) ? 2 : 1), g.cols);
 }
 
 template <class TILE, bool B_KC, bool TINY, Work WORK, class OUT>

@@ -569,6 +569,177 @@ PyObject* combine_vjp(PyObject*, PyObject* const* a, Py_ssize_t count) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- the experts' feed-forward
+using GatedFwdFn = int (*)(const void*, int64_t, int64_t, const void*, const void*, int64_t, int64_t, int64_t, const void*, const void*,
+                           int64_t, int64_t, int64_t, int64_t, int64_t, int, int, void*, void*, void*);
+using GatedVjpFn = int (*)(const void*, int64_t, int64_t, const void*, const void*, int64_t, int64_t, int64_t, const void*, const void*,
+                           int64_t, int64_t, int64_t, int64_t, int64_t, int, int, const void*, const void*, int64_t, void*, void*,
+                           void*, void*, size_t, void*);
+using GatedBytesFn = size_t (*)(int64_t, int64_t, int);
+using QuantiseFn = int (*)(const void*, int64_t, int64_t, int64_t, int, void*, void*, void*);
+using ProductEightFn = int (*)(const void*, int64_t, int64_t, const void*, const void*, int64_t, int64_t, const void*, const void*,
+                               const void*, int64_t, int64_t, int64_t, int64_t, int64_t, int, void*, void*);
+using GatedEightFn = int (*)(const void*, int64_t, int64_t, const void*, const void*, const void*, const void*, const void*, int64_t,
+                             int64_t, const void*, const void*, int64_t, int64_t, int64_t, int64_t, int64_t, int, int, void*, void*);
+
+struct Gated {
+  Product p;
+  const at::Tensor* up;
+  int64_t act;
+};
+// x, w_gate, w_up, offset, source, k, act as binding.py's _gated takes them
+bool gated_args(PyObject* const* a, int device, Gated* g) {
+  PyObject* const args[5] = {a[0], a[1], a[3], a[4], a[5]};
+  if (!product_args(args, device, &g->p) || !integer(a[6], &g->act) || g->act < 0 || g->act > 3) return false;
+  g->up = plain(a[2], device);
+  return g->up != nullptr && g->up->scalar_type() == g->p.w->scalar_type() && g->up->sizes() == g->p.w->sizes() &&
+         g->up->strides() == g->p.w->strides();
+}
+
+// gated_fwd(entry, x, w_gate, w_up, offset, source, k, act, want_pre, stream) -> out or (out, pre)
+PyObject* gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  Here h;
+  Gated g;
+  bool want_pre;
+  if (count != 10 || !here(a[0], a[1], a[9], &h) || !gated_args(a + 1, h.device, &g) || !flag(a[8], &want_pre)) TOPK_NONE;
+  const Product& p = g.p;
+  const auto values = at::TensorOptions().dtype(p.x->scalar_type()).device(p.x->device());
+  at::Tensor out = at::empty({p.slots, p.ho}, values), pre;
+  if (want_pre) pre = at::empty({p.slots, 2, p.ho}, values);
+  const void *xp = data(p.x), *wp = data(p.w), *up = data(g.up), *fp = data(p.offset), *sp = data(p.source);
+  const int64_t stride = p.x->stride(0), m = p.x->size(0);
+  const int type = type_code(*p.x);
+  void *op = out.data_ptr(), *pp = want_pre ? pre.data_ptr() : nullptr;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = reinterpret_cast<GatedFwdFn>(g_entry[h.entry])(xp, stride, m, wp, up, p.w_expert, p.w_out, p.w_in, fp, sp, p.k, p.slots, p.n,
+                                                      p.hi, p.ho, type, int(g.act), op, pp, h.stream);
+  Py_END_ALLOW_THREADS
+  if (outcome(rc, h.entry) != 1) TOPK_NONE;
+  if (!want_pre) return THPVariable_Wrap(out);
+  return tuple_of({THPVariable_Wrap(out), THPVariable_Wrap(pre)});
+  END_HANDLE_TH_ERRORS
+}
+
+// gated_vjp(entry, bytes_entry, x, w_gate, w_up, offset, source, k, act, cotangent, pre, want_x, want_w, stream)
+//   -> (dx or None, dw_gate or None, dw_up or None)
+PyObject* gated_vjp(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  Here h;
+  Gated g;
+  bool want_x, want_w;
+  int64_t bytes_entry;
+  if (count != 14 || !here(a[0], a[2], a[13], &h) || !integer(a[1], &bytes_entry) || bytes_entry < 0 || bytes_entry >= kMaxEntries ||
+      g_entry[bytes_entry] == nullptr || !gated_args(a + 2, h.device, &g) || !flag(a[11], &want_x) || !flag(a[12], &want_w) ||
+      !(want_x || want_w))
+    TOPK_NONE;
+  const Product& p = g.p;
+  const at::Tensor* t = rows_of(a[9], h.device);
+  if (t == nullptr || t->scalar_type() != p.x->scalar_type() || t->size(0) != p.slots || t->size(1) != p.ho) TOPK_NONE;
+  const at::Tensor* pre = a[10] == Py_None ? nullptr : whole(a[10], h.device, p.x->scalar_type(), {p.slots, 2, p.ho});
+  if (a[10] != Py_None && pre == nullptr) TOPK_NONE;
+  const int type = type_code(*p.x);
+  const size_t need = reinterpret_cast<GatedBytesFn>(g_entry[bytes_entry])(p.slots, p.ho, type);
+  if (need > size_t(INT64_MAX)) TOPK_NONE;
+  const auto values = at::TensorOptions().dtype(p.x->scalar_type()).device(p.x->device());
+  at::Tensor dx, dw, du, scratch;
+  if (need > 0) scratch = at::empty({int64_t(need)}, values.dtype(at::kByte));
+  if (want_x) dx = at::empty({p.slots, p.hi}, values);
+  const auto weights = [&]() {
+    return p.w_in == 1 ? at::empty({p.n, p.ho, p.hi}, values) : at::empty({p.n, p.hi, p.ho}, values).transpose(1, 2);
+  };
+  if (want_w) dw = weights(), du = weights();
+  const void *xp = data(p.x), *wp = data(p.w), *up = data(g.up), *fp = data(p.offset), *sp = data(p.source), *tp = data(t),
+             *pp = data(pre);
+  const int64_t stride = p.x->stride(0), m = p.x->size(0), t_stride = t->stride(0);
+  void *dxp = want_x ? dx.data_ptr() : nullptr, *dwp = want_w ? dw.data_ptr() : nullptr, *dup = want_w ? du.data_ptr() : nullptr,
+       *cp = need > 0 ? scratch.data_ptr() : nullptr;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = reinterpret_cast<GatedVjpFn>(g_entry[h.entry])(xp, stride, m, wp, up, p.w_expert, p.w_out, p.w_in, fp, sp, p.k, p.slots, p.n,
+                                                      p.hi, p.ho, type, int(g.act), pp, tp, t_stride, dxp, dwp, dup, cp, need,
+                                                      h.stream);
+  Py_END_ALLOW_THREADS
+  if (outcome(rc, h.entry) != 1) TOPK_NONE;
+  const auto wrapped = [](bool wanted, const at::Tensor& v) {
+    if (wanted) return THPVariable_Wrap(v);
+    Py_INCREF(Py_None);
+    return Py_None;
+  };
+  return tuple_of({wrapped(want_x, dx), wrapped(want_w, dw), wrapped(want_w, du)});
+  END_HANDLE_TH_ERRORS
+}
+
+// quantise(entry, x, stream) -> (q, scale)
+PyObject* quantise(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  Here h;
+  if (count != 3 || !here(a[0], a[1], a[2], &h)) TOPK_NONE;
+  const at::Tensor* x = rows_of(a[1], h.device);
+  if (x == nullptr) TOPK_NONE;
+  const auto bytes = at::TensorOptions().dtype(at::kChar).device(x->device());
+  at::Tensor q = at::empty(x->sizes(), bytes), scale = at::empty({x->size(0)}, bytes.dtype(at::kFloat));
+  const void* xp = x->data_ptr();
+  const int64_t stride = x->stride(0), m = x->size(0), width = x->size(1);
+  const int type = type_code(*x);
+  void *qp = q.data_ptr(), *sp = scale.data_ptr();
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = reinterpret_cast<QuantiseFn>(g_entry[h.entry])(xp, stride, m, width, type, qp, sp, h.stream);
+  Py_END_ALLOW_THREADS
+  if (outcome(rc, h.entry) != 1) TOPK_NONE;
+  return tuple_of({THPVariable_Wrap(q), THPVariable_Wrap(scale)});
+  END_HANDLE_TH_ERRORS
+}
+
+// eight(entry, q, q_scale, w, w_scale, w_up or None, up_scale or None, offset, source, k, act, type code, stream) -> out
+PyObject* eight(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  Here h;
+  int64_t k, act, type;
+  if (count != 13 || !here(a[0], a[1], a[12], &h) || !integer(a[9], &k) || !integer(a[10], &act) || !integer(a[11], &type) ||
+      act < 0 || act > 3 || type < 0 || type > 2)
+    TOPK_NONE;
+  const at::Tensor *q = plain(a[1], h.device), *w = plain(a[3], h.device);
+  if (q == nullptr || q->dim() != 2 || q->scalar_type() != at::kChar || q->stride(1) != 1 || w == nullptr || w->dim() != 3 ||
+      w->scalar_type() != at::kChar || w->size(2) != q->size(1) || w->stride(2) != 1)
+    TOPK_NONE;
+  const int64_t m = q->size(0), n = w->size(0), f = w->size(1), width = w->size(2);
+  const at::Tensor *qs = whole(a[2], h.device, at::kFloat, {m}), *ws = whole(a[4], h.device, at::kFloat, {n, f}), *up = nullptr,
+                   *us = nullptr, *offset = whole(a[7], h.device, at::kInt, {n + 1}), *source = nullptr;
+  if (qs == nullptr || ws == nullptr || offset == nullptr) TOPK_NONE;
+  if (a[5] != Py_None) {
+    up = plain(a[5], h.device), us = whole(a[6], h.device, at::kFloat, {n, f});
+    if (up == nullptr || us == nullptr || up->scalar_type() != at::kChar || up->sizes() != w->sizes() || up->strides() != w->strides())
+      TOPK_NONE;
+  }
+  int64_t slots = m;
+  if (a[8] != Py_None) {
+    source = plain(a[8], h.device);
+    if (source == nullptr || source->dim() != 1 || source->scalar_type() != at::kInt || !source->is_contiguous()) TOPK_NONE;
+    slots = source->size(0);
+  }
+  const at::ScalarType to = type == 0 ? at::kFloat : type == 1 ? at::kBFloat16 : at::kHalf;
+  at::Tensor out = at::empty({slots, f}, at::TensorOptions().dtype(to).device(q->device()));
+  const void *qp = data(q), *qsp = data(qs), *wp = data(w), *wsp = data(ws), *up_p = data(up), *usp = data(us), *fp = data(offset),
+             *sp = data(source);
+  const int64_t stride = q->stride(0), w_expert = w->stride(0), w_out = w->stride(1);
+  void* op = out.data_ptr();
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  if (up == nullptr)
+    rc = reinterpret_cast<ProductEightFn>(g_entry[h.entry])(qp, stride, m, qsp, wp, w_expert, w_out, wsp, fp, sp, k, slots, n, width, f,
+                                                            int(type), op, h.stream);
+  else
+    rc = reinterpret_cast<GatedEightFn>(g_entry[h.entry])(qp, stride, m, qsp, wp, wsp, up_p, usp, w_expert, w_out, fp, sp, k, slots, n,
+                                                          width, f, int(type), int(act), op, h.stream);
+  Py_END_ALLOW_THREADS
+  if (outcome(rc, h.entry) != 1) TOPK_NONE;
+  return THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
 // setup(raw_stream, check, ((name, address), ..)): entry i is the i-th pair
 PyObject* setup(PyObject*, PyObject* args) {
   PyObject *raw, *check, *entries;
@@ -617,6 +788,10 @@ PyMethodDef methods[] = {
     {"product_vjp", reinterpret_cast<PyCFunction>(product_vjp), METH_FASTCALL, nullptr},
     {"combine_fwd", reinterpret_cast<PyCFunction>(combine_fwd), METH_FASTCALL, nullptr},
     {"combine_vjp", reinterpret_cast<PyCFunction>(combine_vjp), METH_FASTCALL, nullptr},
+    {"gated_fwd", reinterpret_cast<PyCFunction>(gated_fwd), METH_FASTCALL, nullptr},
+    {"gated_vjp", reinterpret_cast<PyCFunction>(gated_vjp), METH_FASTCALL, nullptr},
+    {"quantise", reinterpret_cast<PyCFunction>(quantise), METH_FASTCALL, nullptr},
+    {"eight", reinterpret_cast<PyCFunction>(eight), METH_FASTCALL, nullptr},
     {"torch_version", torch_version, METH_NOARGS, nullptr},
     {"setup", setup, METH_VARARGS, nullptr},
     {"workspace_device", workspace_device, METH_O, nullptr},
