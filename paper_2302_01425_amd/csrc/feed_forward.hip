@@ -186,12 +186,29 @@ int launch_gated_vjp(int type, const GatedArgs& g, hipStream_t stream) {
     }
   }
   if (p.dw != nullptr) {
+    // dW has the layout of w: its contiguous direction gives the columns
+    const int64_t apart = stride / 2 * size_of(type);
+    WeightArgs w;
+    const bool x_first = p.w_in != 1;
+    if (x_first)
+      w = {p.x, g.scratch, p.x_stride, stride, p.source, nullptr, divisor(p.k), p.m, p.slots, p.offset, p.slots, p.n, 0, p.h, p.ho,
+           nullptr};
+    else
+      w = {g.scratch, p.x, stride, p.x_stride, nullptr, p.source, divisor(p.k), p.slots, p.m, p.offset, p.slots, p.n, 0, p.ho, p.h,
+           nullptr};
+    const int s = size_of(type);
+    const int64_t tiles = both_weights_tiles(w);
+    const bool whole = s == 2 && p.m > 0 && whole_parts(w.a, w.a_stride, w.m, s) && whole_parts(w.b, w.b_stride, w.cols, s);
+    // (one launch, of a few more workgroups than tiles; products of rows and strides in 32 bits)
+    if (whole && tiles >= 256 && tiles < (int64_t(1) << 22) && w.a_stride < (int64_t(1) << 31) && w.b_stride < (int64_t(1) << 31) &&
+        even_share(p.slots, p.n) >= 1536)
+      return launch_both_weights(type, w, x_first, apart, p.dw, g.dw_up, stream);
     for (int i = 0; i < 2; ++i) {
-      ProductArgs w = p;
-      w.t = static_cast<const char*>(g.scratch) + (i == 0 ? 0 : stride / 2 * size_of(type));
-      w.t_stride = stride;
-      w.dw = i == 0 ? p.dw : g.dw_up;
-      const int launched = launch_product_dw(type, w, stream);
+      ProductArgs q = p;
+      q.t = static_cast<const char*>(g.scratch) + (i == 0 ? 0 : apart);
+      q.t_stride = stride;
+      q.dw = i == 0 ? p.dw : g.dw_up;
+      const int launched = launch_product_dw(type, q, stream);
       if (launched != 0) return launched;
     }
   }

@@ -173,6 +173,25 @@ __device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const Feed
         if constexpr (kOf == 2) load_four(g.u_scale + expert * g.cols + mine + 8 * q, g.cols - mine - 8 * q, us[q]);
       }
     }
+    // cotangents of all blocks at once: the compiler would wait for each block's behind the stores of the one before
+    Packed<T, 4> t[WORK == kSlopes ? MI : 1][4];
+    if constexpr (WORK == kSlopes) {
+      const bool whole = n + 32 <= g.cols;
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const T* row = static_cast<const T*>(g.t) + min(m0 + 32 * i + (lane & 31), m_end - 1) * g.t_stride;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t col = mine + 8 * q;
+          if (whole) {
+            t[i][q] = load_packed<T, 4>(row + col);
+          } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) t[i][q].v[r] = col + r < g.cols ? row[col + r] : T(0.0f);
+          }
+        }
+      }
+    }
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       if (m0 + 32 * i >= m_end) break;
@@ -203,19 +222,12 @@ __device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const Feed
         for (int x = 0; x < 16; ++x) first[x] = act_value<ACT, kFine>(first[x], nullptr) * second[x];
         store_block<OUT>(first, row, inside, there[i], n, n_end);
       } else {
-        const T* t = static_cast<const T*>(g.t) + m * g.t_stride;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float tv[4];
-          load_four(t + mine + 8 * q, there[i] ? g.cols - mine - 8 * q : int64_t(0), tv);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int x = 4 * q + r;
-            float slope;
-            const float value = act_value<ACT, kFine>(first[x], &slope);
-            first[x] = tv[r] * second[x] * slope;
-            second[x] = tv[r] * value;
-          }
+        for (int x = 0; x < 16; ++x) {
+          float slope;
+          const float tv = to_f32(t[i][x / 4].v[x % 4]), value = act_value<ACT, kFine>(first[x], &slope);
+          first[x] = tv * second[x] * slope;
+          second[x] = tv * value;
         }
         // (rounded to the operands' type, which the matrix instructions of the gradients take)
         store_block<OUT>(first, row, inside, there[i], n, n_end);
@@ -253,6 +265,11 @@ int launch_feed_few(const FeedArgs& g, Work work, hipStream_t stream);
 // feed_thin.hpp: few tiles, `narrow` for half as many columns each; otherwise as feed_few.hip
 template <class T>
 int launch_feed_thin(const FeedArgs& g, Work work, bool narrow, hipStream_t stream);
+
+// feed_weights.hip: both weights' gradients of whole, aligned 16-byte parts, not float32.  w: slopes (of the gate) and x, or x and
+// slopes where x_first; few enough tiles for one launch, strides below 2^32 bytes
+int64_t both_weights_tiles(const WeightArgs& g);
+int launch_both_weights(int type, const WeightArgs& w, bool x_first, int64_t apart, void* c, void* c_up, hipStream_t stream);
 
 // elementwise: slopes from the sums that the forward pass kept
 int launch_slopes(int type, const FeedArgs& g, hipStream_t stream);

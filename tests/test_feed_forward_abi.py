@@ -70,7 +70,8 @@ def test_gated(lib):
 
 def test_scratch(lib):
     size = lib.topk_expert_gated_vjp_bytes
-    assert size(8, 4, 0) == 8 * 2 * 4 * 4 and size(8, 5, 0) == 8 * 2 * 8 * 4          # halves of whole 16-byte parts
+    # two halves of whole 16-byte parts per place
+    assert size(8, 4, 0) == 8 * 2 * 4 * 4 and size(8, 5, 0) == 8 * 2 * 8 * 4
     assert size(8, 5, 1) == 8 * 2 * 8 * 2 and size(3, 9, 2) == 3 * 2 * 16 * 2
     assert size(0, 4, 0) == 0 and size(-1, 4, 0) == 0 and size(8, 0, 0) == 0 and size(8, 4, 3) == 0
     assert size(MOST - 1, MOST - 1, 0) == 2 ** 64 - 1                                 # (2^65 bytes: more than there can be)

@@ -159,6 +159,50 @@ def test_large_whole_numbers(gpu, rows, k, n, h, f, dtype):
                 assert torch.equal(dwg[e], (dg.t().contiguous() @ xe).to(dt)) and torch.equal(dwu[e], (du.t().contiguous() @ xe).to(dt)), e
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("h,f", [(1032, 1544), (1280, 1536)])
+@pytest.mark.parametrize("gather", [True, False])
+def test_gradients_of_large_experts(gpu, dtype, h, f, gather):
+    """Some thousand places in two experts, a few in the others, none in one; every ninth place without a row of x, whose cotangent is
+    infinite; x behind the last place and its cotangent hold NaN."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(h)
+    dt = getattr(torch, dtype)
+    at = [0, 3000, 3000, 3001, 8000, 8033]
+    n, slots, m = 5, 8050, 9000
+    share = 10.0 / h ** 0.5
+    x, t = whole((m if gather else slots, h), g, dt, share), whole((slots, f), g, dt, 0.5)
+    offset = torch.tensor(at, dtype=torch.int32, device="cuda")
+    source, gone = None, torch.zeros(slots, dtype=torch.bool, device="cuda")
+    if gather:
+        source = torch.randint(0, 2 * m, (slots,), generator=g, device="cuda", dtype=torch.int32)
+        gone[::9] = True
+        source[::18], source[9::18] = -1, 2 * m + 5
+        t[gone] = float("inf")
+    else:
+        x[at[n]:] = float("nan")
+    t[at[n]:] = float("nan")
+    for turned in (False, True):
+        wg, wu = whole((n, f, h), g, dt, share), whole((n, f, h), g, dt, share)
+        if turned:
+            wg, wu = (w.transpose(1, 2).contiguous().transpose(1, 2) for w in (wg, wu))
+        print("case", dtype, h, f, gather, turned, flush=True)
+        dx = torch.full((slots, h), MARK, device="cuda", dtype=dt)
+        _, dwg, dwu = gpu.topk_expert_gated_vjp(x, wg, wu, offset, t, source=source, k=2, act=gpu.TOPK_ACT_RELU, dx_out=dx)
+        assert (dx[at[n]:] == MARK).all()
+        for e in range(n):
+            part = slice(at[e], at[e + 1])
+            keep = ~gone[part]
+            row = torch.arange(slots, device="cuda")[part] if source is None else torch.where(keep, source[part] // 2, 0).long()
+            xe = x[row].double() * keep[:, None]
+            te = torch.where(keep[:, None], t[part].double(), 0.0)
+            ge, ue = wg[e].double().contiguous(), wu[e].double().contiguous()
+            gs, us = xe @ ge.t().contiguous(), xe @ ue.t().contiguous()
+            dg, du = te * us * (gs > 0), te * gs.clamp(min=0)
+            assert torch.equal(dx[part], (dg @ ge + du @ ue).to(dt)), e
+            assert torch.equal(dwg[e], (dg.t().contiguous() @ xe).to(dt)) and torch.equal(dwu[e], (du.t().contiguous() @ xe).to(dt)), e
+
+
 @pytest.mark.parametrize("rows,k,n,h,f", [(5, 2, 3, 33, 17), (1, 2, 4, 64, 40), (70, 2, 4, 128, 64), (300, 1, 2, 137, 75), (400, 2, 3, 256, 160)])
 @pytest.mark.parametrize("name", ref.ACTS)
 @pytest.mark.parametrize("dtype", DTYPES)
