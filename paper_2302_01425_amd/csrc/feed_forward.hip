@@ -41,7 +41,8 @@ bool whole_parts(const void* p, int64_t stride, int64_t length, int size) {
 //     8 bits, plain: 1 x 8 2048 -> 1024 4.8 / 7.7 / 10.9 / 12.7, 1 x 64 10.2 / 9.3 / 12.7 / 12.1, 8 x 64 39 / 14.9 / 13.3 / 13.5, 32 x 8
 //     24 / 21 / 20 / 16.5, 8 x 8 512 -> 512 6.4 / 5.2 / 6.8 / 6.7; gated: 1 x 8 5.5 / 8.4 / 11.1 / 14.9, 8 x 32 40 / 15.8 / 13.0 / 16.7,
 //     32 x 8 46 / 40 / 35 / 26.
-//   whole parts, 256 x 256: as the products of expert_product.hip.
+//   whole parts, 128 x 128 / 256 x 256: 8 x 250 1000 -> 1500 (96 tiles) 33 / 37, 24 x 125 1024 -> 768 (144) 29 / 33, 5 x 1925 640 ->
+//     1088 (360) 58 / 52, 32 x 512 2048 -> 2048 (1024) 427 / 310.
 template <class T>
 int launch_feed(const FeedArgs& g, bool k_contiguous, Work work, hipStream_t stream) {
   const int64_t share = even_share(g.slots, g.n), experts = min(int64_t(g.n), g.slots);
@@ -68,10 +69,10 @@ int launch_feed(const FeedArgs& g, bool k_contiguous, Work work, hipStream_t str
     const bool whole = g.limit > 0 && whole_parts(g.a, g.a_stride, g.depth, s) &&
                        whole_parts(g.w, g.w_stride, k_contiguous ? g.depth : g.cols, s) && g.w_expert * s % 16 == 0 &&
                        g.apart % 16 == 0 && (g.slots / 256 + g.n) * cut(g.cols, pair ? 128 : 256) < most;
-    if (whole && share >= 96 && row_tiles(g, 256, pair ? 128 : 256) >= 96)
+    if (whole && share >= 96 && row_tiles(g, 256, pair ? 128 : 256) >= 192)
       return launch_feed_large<T>(g, k_contiguous, work, stream);
   }
-  const bool middle = share >= 128 && row_tiles(g, 128, pair ? 64 : 128) >= 200;
+  const bool middle = share >= 96 && row_tiles(g, 128, pair ? 64 : 128) >= 200;
   return launch_feed_tiles<T>(g, k_contiguous, work, middle ? kMiddle : kSmall, stream);
 }
 int launch_type(int type, const FeedArgs& g, bool k_contiguous, Work work, hipStream_t stream) {
