@@ -428,7 +428,7 @@ int topk_combine_vjp(const void* y, int64_t y_stride, const int32_t* slot, const
  * serving products in 8-bit integers.  Places, lists, strides, types and the checks on the device are those above; the last
  * product of a block is topk_expert_product_fwd (rows in expert order).  One expert with offset = (0, rows) is a dense block.
  */
-/* act(g): g / (1 + exp(-g)); g Phi(g), Phi the normal distribution; g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2; max(g, 0) */
+/* act(g): g / (1 + exp(-g)); g Phi(g), Phi the normal distribution; g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2; max(g, 0).  NaN gives NaN */
 enum { TOPK_ACT_SILU = 0, TOPK_ACT_GELU = 1, TOPK_ACT_GELU_TANH = 2, TOPK_ACT_RELU = 3 };
 #define TOPK_I8_WIDTH_MAX 131071    /* terms of a sum of 8-bit products, which is exact in int32 */
 

@@ -1016,19 +1016,19 @@ def topk_quantise_rows(x, q_out=None, scale_out=None, stream=None):
     return _on(x, stream, call)
 
 
-def _eight(q, q_scale, w, w_scale, w_up, up_scale, offset, source, dtype):
-    """Checked arguments of the products in 8 bits: shapes, strides of the weights, the lists."""
+def _eight(q, q_scale, w, w_scale, offset, source, dtype, w_up=None, up_scale=None, pair=False):
+    """Checked arguments of the products in 8 bits, with a pair of weights or one: shapes, strides of the weights, the lists."""
     if not isinstance(q, torch.Tensor) or not q.is_cuda:
         raise TopkError("q must be a tensor in GPU memory")
     if q.dim() != 2 or q.dtype != torch.int8 or (q.shape[1] > 1 and q.stride(1) != 1):
         raise TopkError("q must be a 2-D int8 tensor with contiguous rows")
-    names = ("w", "w_scale") if w_up is None else ("w_gate", "gate_scale")
-    (n, f, h), strides = _pair(w, w if w_up is None else w_up, q, torch.int8, names[0], "w_up")
+    names = ("w_gate", "gate_scale") if pair else ("w", "w_scale")
+    (n, f, h), strides = _pair(w, w_up if pair else w, q, torch.int8, names[0], "w_up")
     if h > 1 and strides[2] != 1:
         raise TopkError(f"{names[0]} must be contiguous along its last dimension")
     _exact(q_scale, (q.shape[0],), _F32, q, "q_scale")
     _exact(w_scale, (n, f), _F32, q, names[1])
-    if w_up is not None:
+    if pair:
         _exact(up_scale, (n, f), _F32, q, "up_scale")
     if dtype not in _TYPES:
         raise TopkError("dtype must be torch.float32, torch.bfloat16 or torch.float16")
@@ -1042,7 +1042,7 @@ def topk_expert_product_i8_fwd(q, q_scale, w, w_scale, offset, source=None, k=1,
         r = _call.eight(_PRODUCT_I8, q, q_scale, w, w_scale, None, None, offset, source, k, 0, _TYPES[dtype], stream)
         if r is not None:
             return r
-    n, ho, h, strides, (slots, off, src) = _eight(q, q_scale, w, w_scale, None, None, offset, source, dtype)
+    n, ho, h, strides, (slots, off, src) = _eight(q, q_scale, w, w_scale, offset, source, dtype)
     if out is not None:
         _exact(out, (slots, ho), dtype, q, "out")
         _apart((("out", out),), (q, q_scale, w, w_scale, offset, source))
@@ -1060,11 +1060,11 @@ def topk_expert_gated_i8_fwd(q, q_scale, w_gate, gate_scale, w_up, up_scale, off
                              dtype=torch.bfloat16, out=None, stream=None):
     """Returns out [slots, f] of dtype: act(g) * u for every place, g and u the products of topk_expert_product_i8_fwd with the two
     weights [n, f, h].  Rows behind offset[n] are not written."""
-    if _call is not None and out is None and dtype in _TYPES:
+    if _call is not None and out is None and dtype in _TYPES and w_up is not None:
         r = _call.eight(_GATED_I8, q, q_scale, w_gate, gate_scale, w_up, up_scale, offset, source, k, act, _TYPES[dtype], stream)
         if r is not None:
             return r
-    n, f, h, strides, (slots, off, src) = _eight(q, q_scale, w_gate, gate_scale, w_up, up_scale, offset, source, dtype)
+    n, f, h, strides, (slots, off, src) = _eight(q, q_scale, w_gate, gate_scale, offset, source, dtype, w_up, up_scale, True)
     if out is not None:
         _exact(out, (slots, f), dtype, q, "out")
         _apart((("out", out),), (q, q_scale, w_gate, gate_scale, w_up, up_scale, offset, source))

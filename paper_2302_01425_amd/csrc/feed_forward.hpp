@@ -96,6 +96,7 @@ __device__ __forceinline__ float inverse(float x) {
 //              (1 / t - 1) / 0.4: off by 8e-9 of it, 3.2e-7 in float32.  g^2 is taken with the rounding it lost.
 //   gelu_tanh  g (1 + tanh z) / 2 = g p(2 z), z = sqrt(2 / pi) (g + 0.044715 g^3)
 //   relu       g where g > 0, slope 0 at 0
+// NaN gives NaN (relu: and the slope 1).
 template <int ACT, bool FINE>
 __device__ __forceinline__ float act_value(float g, float* slope) {
   if constexpr (ACT == kSilu) {
@@ -116,14 +117,14 @@ __device__ __forceinline__ float act_value(float g, float* slope) {
     if (slope != nullptr) *slope = __builtin_fmaf(g * e, 0.398942280f, p);
     return g * p;
   } else if constexpr (ACT == kGeluTanh) {
-    const float b = fminf(fmaxf(g, -30.0f), 30.0f), b2 = b * b;      // (beyond, p is 0 or 1)
+    const float b = g < -30.0f ? -30.0f : g > 30.0f ? 30.0f : g, b2 = b * b;      // (beyond, p is 0 or 1)
     const float z2 = 1.59576912f * b * __builtin_fmaf(0.044715f, b2, 1.0f);
     const float p = inverse<FINE>(1.0f + exp_of<FINE>(-z2));
     if (slope != nullptr) *slope = p + b * p * (1.0f - p) * 1.59576912f * __builtin_fmaf(0.134145f, b2, 1.0f);
     return g * p;
   } else {
-    if (slope != nullptr) *slope = g > 0.0f ? 1.0f : 0.0f;
-    return g > 0.0f ? g : 0.0f;
+    if (slope != nullptr) *slope = g <= 0.0f ? 0.0f : 1.0f;
+    return g <= 0.0f ? 0.0f : g;
   }
 }
 

@@ -10,7 +10,7 @@ def act(name, g):
     """Value and derivative."""
     g = np.asarray(g, np.float64)
     if name == "relu":
-        return np.where(g > 0, g, 0.0), np.where(g > 0, 1.0, 0.0)
+        return np.where(g <= 0, 0.0, g), np.where(g <= 0, 0.0, 1.0)
     if name == "gelu":
         p, d = 0.5 * erfc(-g / np.sqrt(2.0)), np.exp(-0.5 * g * g) / np.sqrt(2.0 * np.pi)
         return g * p, p + g * d

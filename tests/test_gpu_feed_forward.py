@@ -277,7 +277,7 @@ def test_activations_everywhere(gpu, name, dtype):
     small = np.abs(x) < 1e2
     want = value * x
     within(y[small], want[small], (ev * np.abs(x) + (HALF[dtype] + 4 * U) * np.abs(want) + TINY[dtype])[small], "out")
-    assert np.isnan(y[np.isnan(x)]).all() or name == "relu"
+    assert np.isnan(y[np.isnan(x)]).all()
     assert (y[np.isposinf(x)] == np.inf).all()
 
 
@@ -323,6 +323,73 @@ def test_places_without_a_row(gpu, dtype, h, f):
         gpu.topk_expert_gated_vjp(put(x, dtype), put(wg, dtype), put(wu, dtype), o, put(t, dtype), lists[1], 2)
         gpu.topk_expert_gated_vjp(put(x, dtype), put(wg, dtype), put(wu, dtype), o, put(t, dtype), lists[1], 2, pre=pre)
     torch.cuda.synchronize()
+
+
+# every kernel that takes rows of 16 bits: few, thin (of half the columns, and of all), small, middle and large tiles
+KERNELS = [(6, 2, 3, 64, 40), (120, 2, 3, 512, 512), (120, 2, 3, 512, 1024), (300, 2, 2, 129, 1141), (2600, 2, 4, 264, 520), (12000, 2, 8, 1024, 768)]
+
+
+@pytest.mark.parametrize("rows,k,n,h,f", KERNELS)
+@pytest.mark.parametrize("name", ref.ACTS)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_nan_stays_in_its_row(gpu, rows, k, n, h, f, name, dtype):
+    """A NaN in a token makes its places NaN in every output, and nothing else (dW: its experts)."""
+    import torch
+    code = ref.ACTS.index(name)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    dt = getattr(torch, dtype)
+    x = torch.randn((rows, h), generator=g, device="cuda").to(dt)
+    wg, wu = ((torch.randn((n, f, h), generator=g, device="cuda") / h ** 0.5).to(dt) for _ in range(2))
+    idx = torch.rand((rows, n), generator=g, device="cuda").argsort(dim=1)[:, :k].int().contiguous()
+    idx[rows // 2, 0], idx[rows // 2, 1:] = 0, -1                   # the token that is NaN: one place, of the first expert
+    x[rows // 2, h - 1] = float("nan")
+    slot, source, offset, _ = gpu.topk_expert_map(idx, n)
+    t = torch.randn((rows * k, f), generator=g, device="cuda").to(dt)
+    last, mine = int(offset[n]), int(slot[rows // 2, 0])
+    out, pre = gpu.topk_expert_gated_fwd(x, wg, wu, offset, source, k, code, True)
+    for kept in (None, pre):
+        dx, dwg, dwu = gpu.topk_expert_gated_vjp(x, wg, wu, offset, t, source, k, code, kept)
+        for a in (out, pre.flatten(1), dx):
+            bad = torch.isnan(a[:last])
+            assert bad[mine].all() and int(bad.sum()) == a.shape[1]
+        assert torch.isnan(dwg[0]).all() and torch.isnan(dwu[0]).all() and not torch.isnan(dwg[1:]).any() and not torch.isnan(dwu[1:]).any()
+
+
+@pytest.mark.parametrize("rows,k,n,h,f", KERNELS + [(6000, 2, 4, 1032, 1544)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_whatever_lies_behind(gpu, rows, k, n, h, f, dtype):
+    """Scratch that holds NaN, tokens that no place has, and places behind the last, NaN too: outputs as without them, what lies
+    behind the last place as it was."""
+    import ctypes
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(9)
+    dt = getattr(torch, dtype)
+    x = torch.randn((rows, h), generator=g, device="cuda").to(dt)
+    wg, wu = ((torch.randn((n, f, h), generator=g, device="cuda") / h ** 0.5).to(dt) for _ in range(2))
+    idx = torch.rand((rows, n), generator=g, device="cuda").argsort(dim=1)[:, :k].int().contiguous()
+    idx[::7] = -1
+    _, source, offset, _ = gpu.topk_expert_map(idx, n)
+    last, slots = int(offset[n]), rows * k
+    t = torch.randn((slots, f), generator=g, device="cuda").to(dt)
+    want = gpu.topk_expert_gated_vjp(x, wg, wu, offset, t, source, k)
+    y, pre = gpu.topk_expert_gated_fwd(x, wg, wu, offset, source, k, want_pre=True)
+    x[::7], t[last:], source[last:] = float("nan"), float("nan"), 7 * k
+    lib, p = gpu.load(), lambda v: None if v is None else v.data_ptr()
+    need = lib.topk_expert_gated_vjp_bytes(slots, f, DTYPES.index(dtype))
+    kept_want = gpu.topk_expert_gated_vjp(x, wg, wu, offset, t, source, k, pre=pre)
+    pre[last:] = float("nan")
+    for kept, wanted in ((None, want), (pre, kept_want)):
+        scratch = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+        dx, dwg, dwu = torch.full((slots, h), 5.0, device="cuda", dtype=dt), torch.empty_like(wg), torch.empty_like(wu)
+        rc = lib.topk_expert_gated_vjp(p(x), h, rows, p(wg), p(wu), f * h, h, 1, p(offset), p(source), k, slots, n, h, f,
+                                       DTYPES.index(dtype), 0, p(kept), p(t), f, p(dx), p(dwg), p(dwu), p(scratch), need,
+                                       ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+        assert rc == 0
+        assert torch.equal(dx[:last], wanted[0][:last]) and torch.equal(dwg, wanted[1]) and torch.equal(dwu, wanted[2])
+        assert (dx[last:] == 5.0).all()
+    out, sums = torch.full_like(y, 5.0), torch.full_like(pre, 5.0)
+    gpu.topk_expert_gated_fwd(x, wg, wu, offset, source, k, out=out, pre_out=sums)
+    assert torch.equal(out[:last], y[:last]) and torch.equal(sums[:last], pre[:last]) and (out[last:] == 5.0).all() and (sums[last:] == 5.0).all()
 
 
 def test_no_places(gpu):
@@ -740,3 +807,9 @@ def test_refusals(gpu):
     no(lambda: b.topk_expert_gated_i8_fwd(q, s, w8, ws, w8[:, :3], ws, off))
     no(lambda: b.topk_expert_gated_i8_fwd(q, s, w8, ws, w8, ws[:1], off))
     no(lambda: b.topk_expert_gated_i8_fwd(q, s, w8, ws, w8, ws, off, act=7))
+    no(lambda: b.topk_expert_gated_i8_fwd(q, s, w8, ws, None, None, off))
+    no(lambda: b.topk_expert_gated_i8_fwd(q, s, w8, ws, None, ws, off))
+    no(lambda: b.topk_expert_gated_i8_fwd(q, s, w8, ws, w8, None, off))
+    no(lambda: b.topk_expert_gated_fwd(x, w, None, off))
+    no(lambda: b.topk_expert_gated_vjp(x, w, None, off, t))
+    no(lambda: b.topk_expert_gated_vjp(x, w, w, off, None))
