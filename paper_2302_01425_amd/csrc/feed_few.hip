@@ -83,7 +83,8 @@ __device__ __forceinline__ int few_halve(V* v, int lane) {
 }
 
 template <class T, class OUT, Work WORK, int ACT>
-__device__ __forceinline__ void few_store(const FeedArgs& g, int64_t m, int64_t n, bool there, float first, float second) {
+__device__ __forceinline__ void few_store(const FeedArgs& g, int64_t m, int64_t n, bool there, float t, float first,
+                                          float second) {
   constexpr bool kFine = sizeof(OUT) == 4;
   OUT* c = static_cast<OUT*>(g.c) + m * g.c_stride + n;
   if constexpr (WORK == kPlain) {
@@ -98,7 +99,6 @@ __device__ __forceinline__ void few_store(const FeedArgs& g, int64_t m, int64_t 
     }
     *c = from_f32<OUT>(there ? act_value<ACT, kFine>(first, nullptr) * second : 0.0f);
   } else {
-    const float t = there ? to_f32(static_cast<const T*>(g.t)[m * g.t_stride + n]) : 0.0f;
     float slope;
     const float value = act_value<ACT, kFine>(first, &slope);
     c[0] = from_f32<OUT>(there ? t * second * slope : 0.0f);
@@ -131,11 +131,36 @@ __global__ __launch_bounds__(kFewThreads) void feed_few_kernel(FeedArgs g, int t
     if (g.source != nullptr) row = min(int64_t(quotient(max(g.source[row], 0), g.div)), g.limit - 1);
     x[r] = static_cast<const T*>(g.a) + row * g.a_stride;
   }
+  // what a thread needs for the output that it makes of the sums, looked up before them
+  const int i = SHARED ? int(threadIdx.x) : lane, c = i % kOuts;
+  const int64_t m = f.begin + i / kOuts;
+  const bool mine = i < kFewRows * kOuts && m < f.end;
+  bool there = mine;
+  float scale = 0.0f;
+  if (mine) {
+    int64_t row = m;
+    if (g.source != nullptr) {
+      const int pair = g.source[m];
+      row = quotient(max(pair, 0), g.div);
+      there = pair >= 0 && row < g.limit;
+    }
+    if (sizeof(T) == 1 && there) scale = g.a_scale[row];
+  }
   constexpr int64_t kChunk = kWave * N;
   const int64_t group = SHARED ? f.col : f.col * kFewWaves + wave;
   for (int turn = 0; turn < turns; ++turn) {
     const int64_t n0 = (group * turns + turn) * kOuts;
     if (n0 >= g.cols) break;               // (the same for all that share sums)
+    const int64_t n = n0 + c;
+    const bool store = mine && n < g.cols;
+    float first_scale = 0.0f, second_scale = 0.0f, t = 0.0f;
+    if (store && there) {
+      if constexpr (sizeof(T) == 1) {
+        first_scale = g.w_scale[f.expert * g.cols + n];
+        if constexpr (kOf == 2) second_scale = g.u_scale[f.expert * g.cols + n];
+      }
+      if constexpr (WORK == kSlopes) t = to_f32(static_cast<const T*>(g.t)[m * g.t_stride + n]);
+    }
     const T* p[kFewCols];
 #pragma unroll
     for (int c = 0; c < kFewCols; ++c) {
@@ -156,37 +181,24 @@ __global__ __launch_bounds__(kFewThreads) void feed_few_kernel(FeedArgs g, int t
     if ((lane & 3) == 0) sums[set][SHARED ? wave : 0][at] = acc[0];
     if constexpr (SHARED) __syncthreads();               // (and the sums of the turn before are read)
     else meet();
-    const int i = SHARED ? int(threadIdx.x) : lane;
-    if (i < kFewRows * kOuts) {
-      const int r = i / kOuts, c = i % kOuts;
-      const int64_t m = f.begin + r, n = n0 + c;
-      if (m < f.end && n < g.cols) {
-        float v[2] = {0.0f, 0.0f};
+    if (store) {
+      float v[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int o = 0; o < kOf; ++o) {
-          Sum s = 0;
+      for (int o = 0; o < kOf; ++o) {
+        Sum sum = 0;
 #pragma unroll
-          for (int q = 0; q < (SHARED ? kFewWaves : 1); ++q) s += sums[set][q][(c + o * kOuts) * kFewRows + r];
-          v[o] = float(s);
-        }
-        bool there = true;
-        int64_t row = m;
-        if (g.source != nullptr) {
-          const int pair = g.source[m];
-          row = quotient(max(pair, 0), g.div);
-          there = pair >= 0 && row < g.limit;
-        }
-        if constexpr (sizeof(T) == 1) {
-          const float scale = there ? g.a_scale[row] : 0.0f;
-          v[0] = v[0] * scale * g.w_scale[f.expert * g.cols + n];
-          if constexpr (kOf == 2) v[1] = v[1] * scale * g.u_scale[f.expert * g.cols + n];
-        }
-        if constexpr (WORK == kPlain) few_store<T, OUT, WORK, 0>(g, m, n, there, v[0], v[1]);
-        else if (g.act == kSilu) few_store<T, OUT, WORK, kSilu>(g, m, n, there, v[0], v[1]);
-        else if (g.act == kGelu) few_store<T, OUT, WORK, kGelu>(g, m, n, there, v[0], v[1]);
-        else if (g.act == kGeluTanh) few_store<T, OUT, WORK, kGeluTanh>(g, m, n, there, v[0], v[1]);
-        else few_store<T, OUT, WORK, kRelu>(g, m, n, there, v[0], v[1]);
+        for (int q = 0; q < (SHARED ? kFewWaves : 1); ++q) sum += sums[set][q][(c + o * kOuts) * kFewRows + i / kOuts];
+        v[o] = float(sum);
       }
+      if constexpr (sizeof(T) == 1) {
+        v[0] = v[0] * scale * first_scale;
+        if constexpr (kOf == 2) v[1] = v[1] * scale * second_scale;
+      }
+      if constexpr (WORK == kPlain) few_store<T, OUT, WORK, 0>(g, m, n, there, t, v[0], v[1]);
+      else if (g.act == kSilu) few_store<T, OUT, WORK, kSilu>(g, m, n, there, t, v[0], v[1]);
+      else if (g.act == kGelu) few_store<T, OUT, WORK, kGelu>(g, m, n, there, t, v[0], v[1]);
+      else if (g.act == kGeluTanh) few_store<T, OUT, WORK, kGeluTanh>(g, m, n, there, t, v[0], v[1]);
+      else few_store<T, OUT, WORK, kRelu>(g, m, n, there, t, v[0], v[1]);
     }
     if constexpr (!SHARED) meet();
   }

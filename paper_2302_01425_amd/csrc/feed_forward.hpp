@@ -141,39 +141,53 @@ __device__ __forceinline__ void load_four(const T* p, int64_t left, float (&v)[4
   }
 }
 
+// What a wavefront has to know of its rows, from m0 on (below m_end), when it has their sums.  Looked up before the sums: two loads,
+// of which the second needs the first, would otherwise be waited for at the end of every tile.
+template <int MI>
+struct RowsOfTile {
+  bool there[MI];          // the place has a row
+  float scale[MI];         // 8-bit operands
+};
+template <class T, int MI>
+__device__ __forceinline__ RowsOfTile<MI> rows_of_tile(const FeedArgs& g, int64_t m0, int64_t m_end) {
+  RowsOfTile<MI> r;
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int64_t m = m0 + 32 * i + (int(threadIdx.x) & 31);
+    int64_t row = m;
+    r.there[i] = m < m_end;
+    if (r.there[i] && g.source != nullptr) {
+      const int pair = g.source[m];
+      row = quotient(max(pair, 0), g.div);
+      r.there[i] = pair >= 0 && row < g.limit;
+    }
+    r.scale[i] = sizeof(T) == 1 && r.there[i] ? g.a_scale[row] : 0.0f;
+  }
+  return r;
+}
+
 // Sums of a wavefront, MI x NJ blocks of 32 x 32 from row m0 on (below m_end), to the outputs from column n0 on.  Rows whose place
 // has no source are zeros, whatever their operands hold.  Columns from n_end on are left as they were.  T: type of the operands; OUT: of c.
 template <class T, class OUT, Work WORK, int ACT, int MI, int NJ, class ACC>
-__device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const FeedArgs& g, int expert, int64_t m0, int64_t m_end,
-                                            int64_t n0, int64_t n_end) {
+__device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const FeedArgs& g, const RowsOfTile<MI>& rows, int expert,
+                                            int64_t m0, int64_t m_end, int64_t n0, int64_t n_end) {
   constexpr bool kEight = sizeof(T) == 1, kFine = sizeof(OUT) == 4;
   constexpr int kOf = is_pair(WORK) ? 2 : 1;
   const int lane = int(threadIdx.x) & (kWave - 1);
-  bool there[MI];
-  float scale[MI];
+  // (scales of all columns at once, as the cotangents below)
+  float col_scale[kEight ? NJ : 1][4][4];
+  if constexpr (kEight) {
 #pragma unroll
-  for (int i = 0; i < MI; ++i) {
-    const int64_t m = m0 + 32 * i + (lane & 31);
-    int64_t row = m;
-    there[i] = m < m_end;
-    if (there[i] && g.source != nullptr) {
-      const int pair = g.source[m];
-      row = quotient(max(pair, 0), g.div);
-      there[i] = pair >= 0 && row < g.limit;
+    for (int j = 0; j < NJ; ++j) {
+      const int64_t mine = n0 + 32 * (j / kOf) + 4 * (lane >> 5);
+      const float* from = (j % kOf == 0 ? g.w_scale : g.u_scale) + expert * g.cols;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) load_four(from + mine + 8 * q, g.cols - mine - 8 * q, col_scale[j][q]);
     }
-    scale[i] = kEight && there[i] ? g.a_scale[row] : 0.0f;
   }
 #pragma unroll
   for (int j = 0; j < NJ; j += kOf) {
     const int64_t n = n0 + 32 * (j / kOf), mine = n + 4 * (lane >> 5);
-    float ws[4][4], us[4][4];
-    if constexpr (kEight) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        load_four(g.w_scale + expert * g.cols + mine + 8 * q, g.cols - mine - 8 * q, ws[q]);
-        if constexpr (kOf == 2) load_four(g.u_scale + expert * g.cols + mine + 8 * q, g.cols - mine - 8 * q, us[q]);
-      }
-    }
     // cotangents of all blocks at once: the compiler would wait for each block's behind the stores of the one before
     Packed<T, 4> t[WORK == kSlopes ? MI : 1][4];
     if constexpr (WORK == kSlopes) {
@@ -205,23 +219,26 @@ __device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const Feed
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int x = 4 * q + r;
-          first[x] = kEight ? float(acc[i][j][x]) * scale[i] * ws[q][r] : float(acc[i][j][x]);
-          if constexpr (kOf == 2) second[x] = kEight ? float(acc[i][j + 1][x]) * scale[i] * us[q][r] : float(acc[i][j + 1][x]);
+          const auto of = [&](int at) {
+            return kEight ? float(acc[i][at][x]) * rows.scale[i] * col_scale[kEight ? at : 0][q][r] : float(acc[i][at][x]);
+          };
+          first[x] = of(j);
+          if constexpr (kOf == 2) second[x] = of(j + 1);
         }
       }
       if constexpr (kOf == 1) {
-        store_block<OUT>(first, row, inside, there[i], n, n_end);
+        store_block<OUT>(first, row, inside, rows.there[i], n, n_end);
       } else if constexpr (WORK == kOut) {
         if constexpr (!kEight) {
           if (g.pre != nullptr) {
             T* sums = static_cast<T*>(g.pre) + m * 2 * g.cols;
-            store_block<T>(first, sums, inside, there[i], n, n_end);
-            store_block<T>(second, sums + g.cols, inside, there[i], n, n_end);
+            store_block<T>(first, sums, inside, rows.there[i], n, n_end);
+            store_block<T>(second, sums + g.cols, inside, rows.there[i], n, n_end);
           }
         }
 #pragma unroll
         for (int x = 0; x < 16; ++x) first[x] = act_value<ACT, kFine>(first[x], nullptr) * second[x];
-        store_block<OUT>(first, row, inside, there[i], n, n_end);
+        store_block<OUT>(first, row, inside, rows.there[i], n, n_end);
       } else {
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
@@ -231,23 +248,23 @@ __device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const Feed
           second[x] = tv * value;
         }
         // (rounded to the operands' type, which the matrix instructions of the gradients take)
-        store_block<OUT>(first, row, inside, there[i], n, n_end);
-        store_block<OUT>(second, row + g.c_stride / 2, inside, there[i], n, n_end);
+        store_block<OUT>(first, row, inside, rows.there[i], n, n_end);
+        store_block<OUT>(second, row + g.c_stride / 2, inside, rows.there[i], n, n_end);
       }
     }
   }
 }
 
 template <class T, class OUT, Work WORK, int MI, int NJ, class ACC>
-__device__ __forceinline__ void finish_act(const ACC (&acc)[MI][NJ], const FeedArgs& g, int expert, int64_t m0, int64_t m_end,
-                                           int64_t n0, int64_t n_end) {
+__device__ __forceinline__ void finish_act(const ACC (&acc)[MI][NJ], const FeedArgs& g, const RowsOfTile<MI>& rows, int expert,
+                                           int64_t m0, int64_t m_end, int64_t n0, int64_t n_end) {
   if constexpr (!is_pair(WORK)) {
-    finish_tile<T, OUT, WORK, 0>(acc, g, expert, m0, m_end, n0, n_end);
+    finish_tile<T, OUT, WORK, 0>(acc, g, rows, expert, m0, m_end, n0, n_end);
   } else {
-    if (g.act == kSilu) finish_tile<T, OUT, WORK, kSilu>(acc, g, expert, m0, m_end, n0, n_end);
-    else if (g.act == kGelu) finish_tile<T, OUT, WORK, kGelu>(acc, g, expert, m0, m_end, n0, n_end);
-    else if (g.act == kGeluTanh) finish_tile<T, OUT, WORK, kGeluTanh>(acc, g, expert, m0, m_end, n0, n_end);
-    else finish_tile<T, OUT, WORK, kRelu>(acc, g, expert, m0, m_end, n0, n_end);
+    if (g.act == kSilu) finish_tile<T, OUT, WORK, kSilu>(acc, g, rows, expert, m0, m_end, n0, n_end);
+    else if (g.act == kGelu) finish_tile<T, OUT, WORK, kGelu>(acc, g, rows, expert, m0, m_end, n0, n_end);
+    else if (g.act == kGeluTanh) finish_tile<T, OUT, WORK, kGeluTanh>(acc, g, rows, expert, m0, m_end, n0, n_end);
+    else finish_tile<T, OUT, WORK, kRelu>(acc, g, rows, expert, m0, m_end, n0, n_end);
   }
 }
 

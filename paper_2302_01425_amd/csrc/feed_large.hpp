@@ -82,15 +82,17 @@ __global__ __launch_bounds__(kLargeThreads, 1) void feed_large_kernel(FeedArgs g
 #pragma unroll
     for (int i = 0; i < IA::kParts; ++i) a.issue(i, to_a + stage * kStageA);
   };
+  const int wave = int(threadIdx.x) / kWave;
+  const int high = int(f.end - f.begin + 63) / 64;
+  const int wm = (wave & 1) * 32 * high, wn = (wave >> 1) * (kLargeCols / 2);
+  const int64_t m0 = f.begin + wm, m_end = min(f.end, m0 + 32 * high);
   load_b(0);               // (before the rows of A are looked up)
+  const auto rows = rows_of_tile<T, MI>(g, m0, m_end);
   a.load.init_rows(g.a, g.a_stride, WORK == kBoth ? nullptr : g.source, g.div, g.limit, f.begin, f.end);
   load_a(0);
   load_b(1);
   load_a(1);
 
-  const int wave = int(threadIdx.x) / kWave;
-  const int high = int(f.end - f.begin + 63) / 64;
-  const int wm = (wave & 1) * 32 * high, wn = (wave >> 1) * (kLargeCols / 2);
   std::conditional_t<sizeof(T) == 1, i32x16, f32x16> acc[MI][NJ];
   clear(acc);
   wait_stage<IA::kParts + IB::kParts>();
@@ -147,8 +149,7 @@ __global__ __launch_bounds__(kLargeThreads, 1) void feed_large_kernel(FeedArgs g
   else if (high == 2) sum(std::integral_constant<int, 2>{});
   else sum(std::integral_constant<int, 1>{});
   wait_stage<0>();           // (no load may reach LDS that is another workgroup's by then)
-  finish_act<T, OUT, WORK>(acc, g, f.expert, f.begin + wm, min(f.end, f.begin + wm + 32 * high),
-                           n0 + wn / (is_pair(WORK) ? 2 : 1), g.cols);
+  finish_act<T, OUT, WORK>(acc, g, rows, f.expert, m0, m_end, n0 + wn / (is_pair(WORK) ? 2 : 1), g.cols);
 }
 
 template <class T, bool B_KC, Work WORK, class OUT>

@@ -72,6 +72,7 @@ __global__ __launch_bounds__(kThinThreads) void feed_thin_kernel(FeedArgs g) {
     pa[i] = static_cast<const T*>(g.a) + row * g.a_stride + quarter * N;
   }
 
+  const auto rows = rows_of_tile<T, 1>(g, f.begin, f.end);
   Fragment<T> va[kThinSets][kParts][kA], vb[kThinSets][kParts][kB];
   std::conditional_t<sizeof(T) == 1, i32x4, f32x4> sum[kA][kB] = {};
   const auto load = [&](int set, int64_t k0) {
@@ -151,7 +152,7 @@ __global__ __launch_bounds__(kThinThreads) void feed_thin_kernel(FeedArgs g) {
       for (int o = 1; o < kThinWaves; ++o) v += lds[o][col][lane & 31];
       acc[0][j][x] = v;
     }
-  finish_act<T, OUT, WORK>(acc, g, f.expert, f.begin, f.end, n0, min(n0 + kSpan, g.cols));
+  finish_act<T, OUT, WORK>(acc, g, rows, f.expert, f.begin, f.end, n0, min(n0 + kSpan, g.cols));
 }
 
 template <class T, class OUT, Work WORK, int kB>

@@ -70,11 +70,12 @@ __global__ __launch_bounds__(TILE::kThreads, 2) void feed_tiles_kernel(FeedArgs 
   Staged<IB, kInOrder, TINY> b;
   if constexpr (B_KC) b.init_rows(w, g.w_stride, nullptr, Divisor{}, 0, n0, g.cols, apart);
   else b.init_columns(w, g.w_stride, nullptr, n0, g.cols, 0, apart);
+  const auto rows = rows_of_tile<T, TILE::MI>(g, f.begin + TILE::wave_row(), f.end);
   typename TILE::Sums acc;
   clear(acc);
   constexpr int kSums = WORK == kBoth ? 2 : 1;
   sum_steps<TILE, IA, IB, kSums>(lds, a, b, g.depth, g.a_apart / int64_t(sizeof(T)), g.apart / int64_t(sizeof(T)), acc);
-  finish_act<T, OUT, WORK>(acc, g, f.expert, f.begin + TILE::wave_row(), f.end,
+  finish_act<T, OUT, WORK>(acc, g, rows, f.expert, f.begin + TILE::wave_row(), f.end,
                            n0 + TILE::wave_col() / (is_pair(WORK) ? 2 : 1), g.cols);
 }
 
