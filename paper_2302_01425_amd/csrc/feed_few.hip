@@ -169,12 +169,12 @@ __global__ __launch_bounds__(kFewThreads) void feed_few_kernel(FeedArgs g, int t
     }
     Sum acc[kFewCols * kFewRows] = {};
     constexpr int64_t kStride = (SHARED ? kFewWaves : 1) * kChunk;
-    int64_t k0 = SHARED ? wave * kChunk : 0;
-#pragma unroll 2
-    for (; k0 + kChunk <= g.depth; k0 += kStride) few_add<T>(p, x, k0 + lane * N, 0, acc);
-    if (k0 + lane * N < g.depth) {
-      const int64_t k = min(k0 + lane * N, g.depth - N);
-      few_add<T>(p, x, k, int(k0 + lane * N - k), acc);
+    // (one copy of the instructions, which are read from memory by every launch: with two steps at a time and the last by itself one
+    // token of 2048 -> 1024 took 10.5 us in the place of 9.0)
+#pragma unroll 1
+    for (int64_t k = (SHARED ? wave * kChunk : 0) + lane * N; k < g.depth; k += kStride) {
+      const int64_t from = min(k, g.depth - N);
+      few_add<T>(p, x, from, int(k - from), acc);
     }
     const int at = few_halve(acc, lane);
     const int set = SHARED ? turn & 1 : wave;

@@ -1,12 +1,16 @@
 // Rows as 8-bit integers: with a the largest magnitude of a row, scale = a / 127 and q = 127 x / a rounded to the nearest integer,
 // ties to even, of the exact quotient.
 //
-// 127 x / a is taken in float32 as x (127 / a), off by less than 127 * 2^-23; within 2e-5 of a half it is divided in float64, whose
-// quotient of two float32 numbers lies on the same side of every half as the exact one (two such numbers, 24 bits each, are
-// either equal to it or off by at least 2^-33).  One branch for
-// all elements of a part, with float64 for all of them, measured 15 % more.  x is read once, a row stays in the registers of one
-// wavefront or workgroup; rows that do not fit are read twice.  8192 x 2048 bfloat16: 15.8 us, 3.2 TB/s; bound by some 15
-// instructions per element, few rows by the launch.
+// 127 x / a is taken in float32 as v = x (127 / a), off by less than 127 * 2^-23.  Where v is within 2e-5 of a half H, the sign of H a -
+// 127 x decides: with t the float32 product 127 x and t + l the exact one, H a - t is at most 2^-13 a and a multiple of 2^-26 a, so that
+// a fused operation gives it exactly, and subtracting l keeps the sign.  Of 16-bit
+// values one in some 300 is such an element: half of the largest has the quotient 63.5.
+// Rows whose largest magnitude is below 2^-100, where such terms fall out of float32's range, are divided in float64.
+//
+// x is read once, a row stays in the registers of one wavefront or workgroup; rows that do not fit are read twice.  8192 x 4096
+// float32 26.3 us, 6.4 TB/s (partly from the last cache); 8192 x 2048 bfloat16 15.6 us, 3.2 TB/s, bound by some 15 instructions per
+// element; few rows by the launch.  One branch for a part of a row and its elements in float64 together measured 15 % more, float64
+// in a loop over memory 40 % more.
 #include "feed_forward.hpp"
 
 namespace topk {
@@ -16,11 +20,17 @@ constexpr int kThreads = 256;
 constexpr int kHeld = 8;             // parts of 16 bytes of a row that a thread holds
 
 __device__ __forceinline__ int8_t nearest(float x, float a, float r) {
-  const float v = x * r, w = rintf(v);
-  int q = int(w);
-  if (__builtin_expect(!(fabsf(v - w) < 0.5f - 2e-5f), 0)) q = int(rint(127.0 * double(x) / double(a)));
-  return int8_t(q);
+  const float v = x * r;
+  float w = rintf(v);
+  if (__builtin_expect(fabsf(v - w) > 0.5f - 2e-5f, 0)) {
+    const float side = v > w ? 1.0f : -1.0f, t = 127.0f * x, l = __builtin_fmaf(127.0f, x, -t);
+    const float beyond = side * (l - __builtin_fmaf(w + 0.5f * side, a, -t));      // of 127 x behind the half
+    const bool even = rintf(0.5f * w) == 0.5f * w;
+    if (beyond > 0.0f || (beyond == 0.0f && !even)) w += side;
+  }
+  return int8_t(int(w));
 }
+__device__ __forceinline__ int8_t nearest_small(float x, float a) { return int8_t(int(rint(127.0 * double(x) / double(a)))); }
 
 // Of the 16 bytes of a row from element i on, which cross its end: those before it (h >= N).
 template <class T, int N>
@@ -36,10 +46,10 @@ __device__ __forceinline__ uint32_t largest(const Packed<T, N>& p) {
   return top;
 }
 template <class T, int N>
-__device__ __forceinline__ void store_part(int8_t* q, const Packed<T, N>& p, float a, float r, bool finite) {
+__device__ __forceinline__ void store_part(int8_t* q, const Packed<T, N>& p, float a, float r) {
   Packed<int8_t, N> out;
 #pragma unroll
-  for (int j = 0; j < N; ++j) out.v[j] = finite && a > 0.0f ? nearest(to_f32(p.v[j]), a, r) : int8_t(0);
+  for (int j = 0; j < N; ++j) out.v[j] = nearest(to_f32(p.v[j]), a, r);
   store_packed<int8_t, N>(q, out);
 }
 
@@ -81,21 +91,22 @@ __global__ __launch_bounds__(kThreads) void quantise_kernel(QuantiseArgs g, int6
   // (the bits of magnitudes are in their order, infinity behind all numbers and NaN behind it)
   const bool finite = top < 0x7f800000u;
   const float a = __builtin_bit_cast(float, top);
-  // where 127 / a is infinite every element is divided in float64
-  const float r = a < 0x1p-118f ? __builtin_inff() : 127.0f / a;
   if (at == 0) g.scale[row] = finite ? a / 127.0f : __builtin_nanf("");
-  if (tiny) {
-    if (at < g.h) q[at] = finite && a > 0.0f ? nearest(to_f32(x[at]), a, r) : int8_t(0);
+  if (tiny || !finite || a < 0x1p-100f) {
+#pragma unroll 1
+    for (int64_t i = at; i < g.h; i += ALONG) q[i] = finite && a > 0.0f ? nearest_small(to_f32(x[i]), a) : int8_t(0);
     return;
   }
+  const float r = 127.0f / a;
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
     const int64_t p = i * ALONG + at;
-    if (p < parts) store_part<T, N>(q + part_start<T, N>(p * N, g.h), held[i], a, r, finite);
+    if (p < parts) store_part<T, N>(q + part_start<T, N>(p * N, g.h), held[i], a, r);
   }
+#pragma unroll 1
   for (int64_t p = int64_t(kHeld) * ALONG + at; p < parts; p += ALONG) {
     const int64_t i = part_start<T, N>(p * N, g.h);
-    store_part<T, N>(q + i, load_packed<T, N>(x + i), a, r, finite);
+    store_part<T, N>(q + i, load_packed<T, N>(x + i), a, r);
   }
 }
 

@@ -459,6 +459,33 @@ def test_quantise(gpu, m, h, dtype):
         assert np.array_equal(host(s).astype(np.float32), ws.astype(np.float32), equal_nan=True)
 
 
+@pytest.mark.parametrize("h", [64, 513, 2048])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_quantise_beside_halves(gpu, h, dtype):
+    """Quotients at a half and a few steps of the type beside it: 127 x and (H + 1/2) a are exact in float64, and compared."""
+    import torch
+    r = np.random.default_rng(h)
+    m = 300
+    low, high = (-90, 100) if dtype != "float16" else (-8, 12)
+    a = rounded(np.ldexp(1.0 + r.random(m), r.integers(low, high, m)), dtype)
+    half = r.integers(0, 127, (m, h)) + 0.5
+    steps = r.integers(-3, 4, (m, h))
+    x = rounded(half * a[:, None] / 127.0, dtype)
+    x = np.clip(rounded(x * (1.0 + steps * 2 * HALF[dtype]), dtype), 0.0, a[:, None]) * r.choice([-1.0, 1.0], (m, h))
+    x[:, h // 2] = a
+    if dtype != "float32":
+        x[:, ::5] = x[:, ::5] / np.abs(x[:, ::5]) * a[:, None] / 2          # quotient 63.5
+    assert np.array_equal(x, rounded(x, dtype))
+    n = np.floor(127.0 * np.abs(x) / a[:, None] + 0.25)                     # the half beside which it lies, or none near
+    whole = np.rint(127.0 * np.abs(x) / a[:, None])
+    gap = 127.0 * np.abs(x) - (n + 0.5) * a[:, None]
+    near = np.abs(127.0 * np.abs(x) / a[:, None] - (n + 0.5)) < 0.1
+    want = np.where(near, np.where(gap > 0, n + 1, np.where(gap < 0, n, 2 * np.ceil(n / 2))), whole) * np.sign(x)
+    q, scale = gpu.topk_quantise_rows(put(x, dtype))
+    assert np.array_equal(host(q), want)
+    assert np.array_equal(host(scale).astype(np.float32), (a.astype(np.float32) / np.float32(127.0)))
+
+
 def test_quantise_at_the_ends_of_float32(gpu):
     tiny = np.float64(2.0) ** -149
     x = np.array([[tiny, -tiny, 0, 3 * tiny], [2.0 ** -126, 2.0 ** -127, -2.0 ** -130, 0], [3.4e38, -3.4e38, 1e38, 1.0],
