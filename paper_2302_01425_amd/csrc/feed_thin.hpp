@@ -5,6 +5,8 @@
 // and has three of them on their way, straight to the registers that the matrix instructions read, without LDS or barriers.  The
 // instructions of 16 x 16 outputs have 64 bytes of k of 16 rows at a time, so that a load reads 16 runs of 64 bytes (those of 32 x
 // 32 outputs would read 32 runs of 32, and the first cache takes as long for each).  The wavefronts' sums meet in LDS.
+//
+// Gated, bfloat16: 32 x 8 places, 2048 -> 1024: 51 us, 5.3 TB/s of W, bound by HBM (64 rows per tile: 68); 1 x 32 12.2 us.
 #pragma once
 
 #include "feed_forward.hpp"

@@ -5,6 +5,10 @@
 // stages of 32 KB, so that a step's loads have three steps to arrive.  The gate's and the up projection's tiles are dealt as those of
 // one array, every die an eighth of every expert's (split_tiles).  Slopes of a place without a row of x are zeros; its row of x,
 // and what lies behind an expert's last place, is read as zeros.
+//
+// Half as many operand bytes per output as tiles of 128 x 256, but nothing overlaps a tile's stores, so for experts of many places: both
+// weights of 8192 x 4096 from 8192 places 865 us (1.27 PFLOP/s), with the other tiles 1028; 32 experts of 512 places, 2048 x 2048, 490
+// and 455.
 #include "feed_forward.hpp"
 
 namespace topk {

@@ -569,7 +569,7 @@ PyObject* combine_vjp(PyObject*, PyObject* const* a, Py_ssize_t count) {
   END_HANDLE_TH_ERRORS
 }
 
-// ---- the experts' feed-forward
+// ---- the experts' feed-forward (one token, gated, in 8 bits: 10.5 us for both calls, 14 by the checks of binding.py)
 using GatedFwdFn = int (*)(const void*, int64_t, int64_t, const void*, const void*, int64_t, int64_t, int64_t, const void*, const void*,
                            int64_t, int64_t, int64_t, int64_t, int64_t, int, int, void*, void*, void*);
 using GatedVjpFn = int (*)(const void*, int64_t, int64_t, const void*, const void*, int64_t, int64_t, int64_t, const void*, const void*,
