@@ -613,6 +613,89 @@ def test_rows_of_nan_in_8_bits(gpu):
         assert torch.isnan(out[[2, 5]]).all() and not torch.isnan(out[[0, 1, 3, 4, 6, 7]]).any() and (out[[3, 6, 7]] == 0).all()
 
 
+# ---- offsets that 32 bits do not hold --------------------------------------------------------------------------------------
+
+def small_whole(shape, dtype, seed, share=1.0):
+    """-1, 0 and 1, of which the fraction `share` is not cleared."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    v = torch.empty(shape, dtype=torch.int8, device="cuda").random_(-1, 2, generator=g)
+    if share < 1.0:
+        v *= torch.empty(shape, dtype=torch.int8, device="cuda").random_(0, int(1 / share), generator=g) == 0
+    return v.to(dtype)
+
+
+def test_many_places_of_wide_rows(gpu):
+    """2.3e9 outputs, twice as many kept sums and slopes: the last expert's places as by themselves."""
+    import torch
+    slots, h, f, relu = 140000, 16, 16384, gpu.TOPK_ACT_RELU
+    x, t = small_whole((slots, h), torch.bfloat16, 1), small_whole((slots, f), torch.bfloat16, 2)
+    wg, wu = small_whole((3, f, h), torch.bfloat16, 3), small_whole((3, f, h), torch.bfloat16, 4)
+    off = torch.tensor([0, 60000, 60000, slots], dtype=torch.int32, device="cuda")
+    out, pre = gpu.topk_expert_gated_fwd(x, wg, wu, off, act=relu, want_pre=True)
+    last = slice(slots - 3000, slots)
+    alone = torch.tensor([0, 3000], dtype=torch.int32, device="cuda")
+    want, sums = gpu.topk_expert_gated_fwd(x[last], wg[2:], wu[2:], alone, act=relu, want_pre=True)
+    assert torch.equal(out[last], want) and torch.equal(pre[last], sums)
+    del out
+    wants = gpu.topk_expert_gated_vjp(x[last], wg[2:], wu[2:], alone, t[last], act=relu)
+    for kept in (None, pre):
+        dx, dwg, dwu = gpu.topk_expert_gated_vjp(x, wg, wu, off, t, act=relu, pre=kept)
+        assert torch.equal(dx[last], wants[0])
+        # sums of whole numbers below 2^24, in any order
+        g, u = (x[60000:].float() @ w[2].float().t().contiguous() for w in (wg, wu))
+        tf = t[60000:].float()
+        assert torch.equal(dwu[2], ((tf * g.clamp(min=0)).t().contiguous() @ x[60000:].float()).bfloat16())
+        assert torch.equal(dwg[2], ((tf * u * (g > 0)).t().contiguous() @ x[60000:].float()).bfloat16())
+        assert (dwg[1] == 0).all() and (dwu[1] == 0).all()
+        del g, u, tf
+
+
+@pytest.mark.parametrize("places", [5, 100, 700])
+def test_rows_and_weights_far_apart(gpu, places):
+    """Tokens of 2.2e9 values, weights of 2.7e9: rows at the end, by experts at the end, as by themselves; 16 and 8 bits."""
+    import torch
+    m, h, n, f, relu = 270000, 8192, 40, 8192, gpu.TOPK_ACT_RELU
+    g = torch.Generator(device="cuda").manual_seed(places)
+    rows = m - 1 - torch.randperm(2000, generator=g, device="cuda")[:places]
+    source = (2 * rows + 1).int()
+    off = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    off[n - 1], off[n] = places // 3, places
+    alone = off[n - 2:].contiguous()
+    t = small_whole((places, f), torch.bfloat16, 3)
+    for dtype in (torch.bfloat16, torch.int8):
+        x = torch.zeros((m, h), dtype=dtype, device="cuda")
+        x[-2000:] = small_whole((2000, h), dtype, 1, 0.01)
+        wg, wu = (torch.zeros((n, f, h), dtype=dtype, device="cuda") for _ in range(2))
+        wg[n - 2:], wu[n - 2:] = small_whole((2, f, h), dtype, 4), small_whole((2, f, h), dtype, 5)
+        if dtype == torch.int8:
+            one, each = torch.ones(m, device="cuda"), torch.ones((n, f), device="cuda")
+            got = gpu.topk_expert_gated_i8_fwd(x, one, wg, each, wu, each, off, source, 2, relu, torch.float32)
+            want = gpu.topk_expert_gated_i8_fwd(x[rows], one[:places], wg[n - 2:], each[:2], wu[n - 2:], each[:2], alone, None, 1, relu,
+                                                torch.float32)
+            assert torch.equal(got, want) and (want != 0).any()
+            got = gpu.topk_expert_product_i8_fwd(x, one, wg, each, off, source, 2, torch.float32)
+            assert torch.equal(got, gpu.topk_expert_product_i8_fwd(x[rows], one[:places], wg[n - 2:], each[:2], alone, dtype=torch.float32))
+        else:
+            got = gpu.topk_expert_gated_fwd(x, wg, wu, off, source, 2, relu)
+            want = gpu.topk_expert_gated_fwd(x[rows], wg[n - 2:], wu[n - 2:], alone, None, 1, relu)
+            assert torch.equal(got, want) and (want != 0).any()
+            back = gpu.topk_expert_gated_vjp(x, wg, wu, off, t, source, 2, relu)
+            wants = gpu.topk_expert_gated_vjp(x[rows], wg[n - 2:], wu[n - 2:], alone, t, None, 1, relu)
+            assert torch.equal(back[0], wants[0])
+            for a, b in zip(back[1:], wants[1:]):
+                assert torch.equal(a[n - 2:], b) and not a[:n - 2].any()
+
+
+def test_rows_in_8_bits_far_apart(gpu):
+    import torch
+    x = torch.zeros((270000, 8192), dtype=torch.bfloat16, device="cuda")
+    x[-3:] = torch.randn((3, 8192), device="cuda").bfloat16()
+    q, scale = gpu.topk_quantise_rows(x)
+    q0, s0 = gpu.topk_quantise_rows(x[-3:].clone())
+    assert torch.equal(q[-3:], q0) and torch.equal(scale[-3:], s0) and not q[:-3].any() and not scale[:-3].any()
+
+
 # ---- together, captured, elsewhere -----------------------------------------------------------------------------------------
 
 def layer(gpu, x, logits, wg, wu, wd, k):
