@@ -41,6 +41,11 @@ bool whole_parts(const void* p, int64_t stride, int64_t length, int size) {
 //     8 bits, plain: 1 x 8 2048 -> 1024 4.8 / 7.7 / 10.9 / 12.7, 1 x 64 10.2 / 9.3 / 12.7 / 12.1, 8 x 64 39 / 14.9 / 13.3 / 13.5, 32 x 8
 //     24 / 21 / 20 / 16.5, 8 x 8 512 -> 512 6.4 / 5.2 / 6.8 / 6.7; gated: 1 x 8 5.5 / 8.4 / 11.1 / 14.9, 8 x 32 40 / 15.8 / 13.0 / 16.7,
 //     32 x 8 46 / 40 / 35 / 26.
+//   W with one row per k, 32 rows of half the columns / of all / 64 rows (us, turned weights; dx of kept sums): float32 1 x 1 2048 -> 1024
+//     24 / 39 / 94; 26 / 40 / 68, 8 x 32 41 / 47 / 104; 46 / 51 / 82, 8 x 64 (256 tiles of all) 68 / 47 / 104; 66 / 52 / 84, 32 x 8 117 /
+//     104 / 165; 126 / 108 / 189, 32 x 64 (1024) 241 / 177 / 177; 236 / 188 / 211, 8 x 250 1000 -> 1500 (1536; 512) 164 / 134 / 132; 162 /
+//     140 / 163.  bfloat16 1 x 1 2048 -> 1024 18.3 / 32 / 24; 19.8 / 33 / 24, 8 x 1 (128) 28.7 / 49 / 33; 29.4 / 49 / 31, 8 x 64 43 / 50 / 36;
+//     37 / 50 / 33, 8 x 32 1001 -> 301 15 / 22 / 18; 12.6 / 18 / 14.
 //   whole parts, 128 x 128 / 256 x 256: 8 x 250 1000 -> 1500 (96 tiles) 33 / 37, 24 x 125 1024 -> 768 (144) 29 / 33, 5 x 1925 640 ->
 //     1088 (360) 58 / 52, 32 x 512 2048 -> 2048 (1024) 427 / 310.
 template <class T>
@@ -64,6 +69,13 @@ int launch_feed(const FeedArgs& g, bool k_contiguous, Work work, hipStream_t str
     const bool thin = s == 1 ? tiles < 300 : s == 2 ? tiles < 768 || (tiles <= 1024 && share <= 16)
                                                     : tiles < 1024 || (tiles == 1024 && share <= 32);
     if (aligned && thin) return launch_feed_thin<T>(g, work, false, stream);
+  }
+  if constexpr (s > 1) {
+    const int64_t tiles = experts * cut(share, 32) * cut(g.cols, pair ? 64 : 128);
+    const bool narrow = s == 2 || tiles <= 128;
+    if (!k_contiguous && g.limit > 0 && g.depth * s >= 16 && g.cols >= (pair ? 64 : 128) / (narrow ? 2 : 1) &&
+        tiles <= (s == 4 ? 1024 : 128) && (g.slots / 4 + g.n) * cut(g.cols, 2) < most)
+      return launch_feed_across<T>(g, work, narrow, stream);
   }
   if constexpr (s < 4) {
     const bool whole = g.limit > 0 && whole_parts(g.a, g.a_stride, g.depth, s) &&

@@ -284,6 +284,11 @@ int launch_feed_few(const FeedArgs& g, Work work, hipStream_t stream);
 template <class T>
 int launch_feed_thin(const FeedArgs& g, Work work, bool narrow, hipStream_t stream);
 
+// feed_across.hpp: few tiles, W contiguous in n, limit > 0, 16 bytes of k and 128 columns (64 of a pair) at least, `narrow` half as
+// many; not 8 bits
+template <class T>
+int launch_feed_across(const FeedArgs& g, Work work, bool narrow, hipStream_t stream);
+
 // feed_weights.hip: both weights' gradients of whole, aligned 16-byte parts, not float32.  w: slopes (of the gate) and x, or x and
 // slopes where x_first; few enough tiles for one launch, strides below 2^32 bytes
 int64_t both_weights_tiles(const WeightArgs& g);

@@ -392,6 +392,26 @@ def test_whatever_lies_behind(gpu, rows, k, n, h, f, dtype):
     assert torch.equal(out[:last], y[:last]) and torch.equal(sums[:last], pre[:last]) and (out[last:] == 5.0).all() and (sums[last:] == 5.0).all()
 
 
+# W with one row per k (turned weights, dx): widths at which its tiles of 32, 64 and 128 columns end, overlap or do not fit, depths at
+# which a step of 8 or 16, times four wavefronts, and the parts of it end
+@pytest.mark.parametrize("h,f", [(31, 33), (32, 31), (64, 32), (65, 64), (127, 65), (129, 127), (4, 128), (9, 130), (263, 96), (520, 257)])
+@pytest.mark.parametrize("rows", [1, 33, 100])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_one_row_per_k(gpu, rows, h, f, dtype):
+    (x, wg, wu, t), (xd, gd, ud, td), k, source, offset = case(rows, 2, 3, h, f, dtype, True, True, rows + h + f, True)
+    sd, od, end = put(source, "int32"), put(offset, "int32"), offset[-1]
+    out, pre = gpu.topk_expert_gated_fwd(xd, gd, ud, od, sd, 2, gpu.TOPK_ACT_RELU, True)
+    want, g, u = ref.gated(x, wg, wu, offset, source, 2, "relu")
+    assert np.nanmax(np.abs(np.concatenate((g, u, np.zeros((1, f)))))) < 256
+    assert np.array_equal(host(out)[:end], rounded(want[:end], dtype)) and np.array_equal(host(pre)[:end, 0], g[:end])
+    wants = ref.gated_vjp(x, wg, wu, offset, source, 2, "relu", t)
+    for weights in ((gd, ud), (gd.contiguous(), ud.contiguous())):
+        for kept in (None, pre):
+            got = gpu.topk_expert_gated_vjp(xd, *weights, od, td, sd, 2, gpu.TOPK_ACT_RELU, kept)
+            assert np.array_equal(host(got[0])[:end], rounded(wants[0][:end], dtype))
+            assert np.array_equal(host(got[1]), rounded(wants[1], dtype)) and np.array_equal(host(got[2]), rounded(wants[2], dtype))
+
+
 def test_no_places(gpu):
     import torch
     w, x, off = torch.randn((3, 5, 4), device="cuda"), torch.empty((0, 4), device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
