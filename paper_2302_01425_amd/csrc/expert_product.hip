@@ -65,7 +65,7 @@ int launch_product_dx(int type, const ProductArgs& p, hipStream_t stream) {
   return launch_rows(type, g, p.w_out == 1, stream);
 }
 
-int launch_product_dw(int type, const ProductArgs& p, hipStream_t stream) {
+int launch_product_dw(int type, const ProductArgs& p, hipStream_t stream, int64_t apart, void* dw_up) {
   // dW has the layout of w: its contiguous direction gives the columns
   WeightArgs g;
   if (p.w_in == 1)
@@ -74,6 +74,8 @@ int launch_product_dw(int type, const ProductArgs& p, hipStream_t stream) {
   else
     g = {p.x, p.t, p.x_stride, p.t_stride, p.source, nullptr, divisor(p.k), p.m, p.slots, p.offset, p.slots, p.n, 0, p.h, p.ho,
          p.dw};
+  g.stacked = p.w_in == 1 ? 1 : 2, g.apart = apart, g.c_up = dw_up;
+  const int64_t arrays = dw_up != nullptr ? 2 : 1;
   const int s = size_of(type);
   const bool whole = whole_parts(g.a, g.a_stride, g.m, s) && whole_parts(g.b, g.b_stride, g.cols, s) &&
                      g.a_stride * s < (int64_t(1) << 32) && g.b_stride * s < (int64_t(1) << 32);   // (32-bit products of rows)
@@ -81,8 +83,8 @@ int launch_product_dw(int type, const ProductArgs& p, hipStream_t stream) {
   // of 128, 1024 x 1024, 256 tiles: 19 / 15.  Others, 64 x 64 / 128 x 128: 1025 x 2047, 64 experts of 32 rows 190 / 160, of 256
   // 374 / 271; 4 of 139 rows, 1501 x 1501, 576 tiles 20 / 19; 40 of 70, 777 x 333, 840 tiles 23 / 23; 10 of 300, 515 x 1001, 400
   // tiles 24 / 29.
-  if (whole && p.n * cut(g.m, 128) * cut(g.cols, 256) >= 256) return launch_weight_tiles(type, g, kWideDirect, stream);
-  return launch_weight_tiles(type, g, p.n * cut(g.m, 128) * cut(g.cols, 128) >= 600 ? kMiddle : kSmall, stream);
+  if (whole && apart % 16 == 0 && arrays * p.n * cut(g.m, 128) * cut(g.cols, 256) >= 256) return launch_weight_tiles(type, g, kWideDirect, stream);
+  return launch_weight_tiles(type, g, arrays * p.n * cut(g.m, 128) * cut(g.cols, 128) >= 600 ? kMiddle : kSmall, stream);
 }
 
 }  // namespace topk

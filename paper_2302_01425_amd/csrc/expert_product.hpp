@@ -171,6 +171,11 @@ struct WeightArgs {
   void* c;
   // tiles, and those of a die (split_tiles)
   int64_t m_tiles = 0, col_tiles = 0, die_m = 0, die_cols = 0;
+  // a second array of the same kind, c_up, of which one operand lies `apart` bytes behind the first's: the tiles of both as those of
+  // one array, A's side (stacked 1) or B's (2) twice as long; tiles of one along that side
+  int stacked = 0;
+  int64_t apart = 0, one = 0;
+  void* c_up = nullptr;
 };
 // Every die gets an eighth of every expert's tiles, since experts differ in their rows: a rectangle of the tiles, that of 1 x 8, 2 x
 // 4, 4 x 2 or 8 x 1 such rectangles that reads least, or an eighth of the tiles in row order (die_cols 0) where rectangles would

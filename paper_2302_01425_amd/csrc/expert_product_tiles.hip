@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_tiles_kernel(RowsArgs g) {
 
 // LIST: which operand's rows are found through source (0: neither, 1: A, 2: B)
 enum Load { kDirect, kStaged, kTiny };
-template <class TILE, int LIST, Load LOAD>
+template <class TILE, int LIST, Load LOAD, bool BOTH>
 __global__ __launch_bounds__(kThreads, 2) void weight_tiles_kernel(WeightArgs g) {
   using T = typename TILE::T;
   __shared__ __attribute__((aligned(1024))) char lds[(LOAD == kDirect ? 3 : 2) * TILE::kStageBytes];
@@ -145,10 +145,22 @@ __global__ __launch_bounds__(kThreads, 2) void weight_tiles_kernel(WeightArgs g)
   int64_t begin, end;
   places(g.offset, e, g.slots, &begin, &end);
   T* c = static_cast<T*>(g.c) + e * g.m * g.cols;
+  const char *from_a = static_cast<const char*>(g.a), *from_b = static_cast<const char*>(g.b);
+  int64_t m_tiles = g.m_tiles, col_tiles = g.col_tiles;
+  if constexpr (BOTH) {
+    const bool rows_twice = g.stacked == 1;
+    int64_t& at = rows_twice ? m0 : n0;
+    (rows_twice ? m_tiles : col_tiles) = g.one;
+    if (at >= g.one) {
+      at -= g.one;
+      (rows_twice ? from_a : from_b) += g.apart;
+      c = static_cast<T*>(g.c_up) + e * g.m * g.cols;
+    }
+  }
   // An expert without places: zeros as one run, not in tiles, whose rows begin and end inside cache lines (31 experts of 2950 x 2919,
   // 534 MB, three of them with one place: 108 us, in tiles 182)
   if (begin == end) {
-    store_zeros<kThreads>(c, g.m * g.cols, m0 * g.col_tiles + n0, g.m_tiles * g.col_tiles);
+    store_zeros<kThreads>(c, g.m * g.cols, m0 * col_tiles + n0, m_tiles * col_tiles);
     return;
   }
   m0 = LOAD == kDirect ? m0 * TILE::kRows : tile_start(m0, TILE::kRows, g.m);
@@ -158,9 +170,9 @@ __global__ __launch_bounds__(kThreads, 2) void weight_tiles_kernel(WeightArgs g)
   constexpr Order kOrderA = LIST == 0 ? kInOrder : LIST == 1 ? kListed : kInOrderWhereListed;
   constexpr Order kOrderB = LIST == 0 ? kInOrder : LIST == 2 ? kListed : kInOrderWhereListed;
   std::conditional_t<LOAD == kDirect, Direct<IA, kOrderA>, Staged<IA, kOrderA, LOAD == kTiny>> a;
-  a.init_columns(g.a, g.a_stride, rows, m0, g.m, begin);
+  a.init_columns(from_a, g.a_stride, rows, m0, g.m, begin);
   std::conditional_t<LOAD == kDirect, Direct<IB, kOrderB>, Staged<IB, kOrderB, LOAD == kTiny>> b;
-  b.init_columns(g.b, g.b_stride, rows, n0, g.cols, begin);
+  b.init_columns(from_b, g.b_stride, rows, n0, g.cols, begin);
   typename TILE::Sums acc;
   clear(acc);
   const Table table{rows, there, LIST == 0 ? nullptr : (LIST == 1 ? g.a_source : g.b_source) + begin, g.div,
@@ -179,15 +191,28 @@ int rows_tile(RowsArgs g, bool k_contiguous, hipStream_t stream) {
   });
 }
 
-template <class TILE, Load LOAD>
-int weight_tile(WeightArgs g, hipStream_t stream) {
-  const int64_t blocks = split_tiles(&g, TILE::kRows, TILE::kCols);
+template <class TILE, Load LOAD, bool BOTH>
+int weight_tile_of(const WeightArgs& g, int64_t blocks, hipStream_t stream) {
   return in_launches<kThreads>(g, blocks, [&](const WeightArgs& part, dim3 grid) {
     const dim3 block(kThreads);
-    if (part.a_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 1, LOAD>), grid, block, 0, stream, part);
-    else if (part.b_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 2, LOAD>), grid, block, 0, stream, part);
-    else hipLaunchKernelGGL((weight_tiles_kernel<TILE, 0, LOAD>), grid, block, 0, stream, part);
+    if (part.a_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 1, LOAD, BOTH>), grid, block, 0, stream, part);
+    else if (part.b_source != nullptr) hipLaunchKernelGGL((weight_tiles_kernel<TILE, 2, LOAD, BOTH>), grid, block, 0, stream, part);
+    else hipLaunchKernelGGL((weight_tiles_kernel<TILE, 0, LOAD, BOTH>), grid, block, 0, stream, part);
   });
+}
+template <class TILE, Load LOAD>
+int weight_tile(WeightArgs g, hipStream_t stream) {
+  if (g.c_up == nullptr) {
+    const int64_t blocks = split_tiles(&g, TILE::kRows, TILE::kCols);
+    return weight_tile_of<TILE, LOAD, false>(g, blocks, stream);
+  }
+  WeightArgs all = g;
+  const int64_t m_tiles = (g.m + TILE::kRows - 1) / TILE::kRows, col_tiles = (g.cols + TILE::kCols - 1) / TILE::kCols;
+  g.one = g.stacked == 1 ? m_tiles : col_tiles;
+  all.m = m_tiles * TILE::kRows * (g.stacked == 1 ? 2 : 1), all.cols = col_tiles * TILE::kCols * (g.stacked == 1 ? 1 : 2);
+  const int64_t blocks = split_tiles(&all, TILE::kRows, TILE::kCols);
+  g.m_tiles = all.m_tiles, g.col_tiles = all.col_tiles, g.die_m = all.die_m, g.die_cols = all.die_cols;
+  return weight_tile_of<TILE, LOAD, true>(g, blocks, stream);
 }
 template <class T>
 int rows_type(const RowsArgs& g, bool k_contiguous, TileKind kind, hipStream_t stream) {

@@ -76,7 +76,8 @@ struct ProductArgs {
 };
 int launch_product_fwd(int type, const ProductArgs& a, hipStream_t stream);
 int launch_product_dx(int type, const ProductArgs& a, hipStream_t stream);
-int launch_product_dw(int type, const ProductArgs& a, hipStream_t stream);
+// (with dw_up: also that of a second cotangent, `apart` bytes behind the first, in the same launch)
+int launch_product_dw(int type, const ProductArgs& a, hipStream_t stream, int64_t apart = 0, void* dw_up = nullptr);
 
 struct CombineArgs {
   const void* y;             // [slots][h]

@@ -217,14 +217,9 @@ int launch_gated_vjp(int type, const GatedArgs& g, hipStream_t stream) {
     if (whole && tiles >= 256 && tiles < (int64_t(1) << 22) && w.a_stride < (int64_t(1) << 31) && w.b_stride < (int64_t(1) << 31) &&
         even_share(p.slots, p.n) >= 1536)
       return launch_both_weights(type, w, x_first, apart, p.dw, g.dw_up, stream);
-    for (int i = 0; i < 2; ++i) {
-      ProductArgs q = p;
-      q.t = static_cast<const char*>(g.scratch) + (i == 0 ? 0 : apart);
-      q.t_stride = stride;
-      q.dw = i == 0 ? p.dw : g.dw_up;
-      const int launched = launch_product_dw(type, q, stream);
-      if (launched != 0) return launched;
-    }
+    ProductArgs q = p;
+    q.t = g.scratch, q.t_stride = stride;
+    return launch_product_dw(type, q, stream, apart, g.dw_up);
   }
   return 0;
 }
