@@ -7,8 +7,8 @@
 // and what lies behind an expert's last place, is read as zeros.
 //
 // Half as many operand bytes per output as tiles of 128 x 256, but nothing overlaps a tile's stores, so for experts of many places: both
-// weights of 8192 x 4096 from 8192 places 865 us (1.27 PFLOP/s), with the other tiles 1028; 32 experts of 512 places, 2048 x 2048, 490
-// and 455.
+// weights of 8192 x 4096 from 8192 places 865 us (1.27 PFLOP/s), with the other tiles, a launch per weight, 1028; 32 experts of 512
+// places, 2048 x 2048, 490 and 455 (390 with the others' in one launch).
 #include "feed_forward.hpp"
 
 namespace topk {
