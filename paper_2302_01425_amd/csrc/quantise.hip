@@ -5,7 +5,7 @@
 // 127 x decides: with t the float32 product 127 x and t + l the exact one, H a - t is at most 2^-13 a and a multiple of 2^-26 a, so that
 // a fused operation gives it exactly, and subtracting l keeps the sign.  Of 16-bit
 // values one in some 300 is such an element: half of the largest has the quotient 63.5.
-// Rows whose largest magnitude is below 2^-100, where such terms fall out of float32's range, are divided in float64.
+// Rows whose largest magnitude is below 2^-100 or above 2^120, where such terms fall out of float32's range, are divided in float64.
 //
 // x is read once, a row stays in the registers of one wavefront or workgroup; rows that do not fit are read twice.  8192 x 4096
 // float32 26.3 us, 6.4 TB/s (partly from the last cache); 8192 x 2048 bfloat16 15.6 us, 3.2 TB/s, bound by some 15 instructions per
@@ -30,7 +30,7 @@ __device__ __forceinline__ int8_t nearest(float x, float a, float r) {
   }
   return int8_t(int(w));
 }
-__device__ __forceinline__ int8_t nearest_small(float x, float a) { return int8_t(int(rint(127.0 * double(x) / double(a)))); }
+__device__ __forceinline__ int8_t nearest_divided(float x, float a) { return int8_t(int(rint(127.0 * double(x) / double(a)))); }
 
 // Of the 16 bytes of a row from element i on, which cross its end: those before it (h >= N).
 template <class T, int N>
@@ -92,9 +92,9 @@ __global__ __launch_bounds__(kThreads) void quantise_kernel(QuantiseArgs g, int6
   const bool finite = top < 0x7f800000u;
   const float a = __builtin_bit_cast(float, top);
   if (at == 0) g.scale[row] = finite ? a / 127.0f : __builtin_nanf("");
-  if (tiny || !finite || a < 0x1p-100f) {
+  if (tiny || !finite || a < 0x1p-100f || a > 0x1p120f) {
 #pragma unroll 1
-    for (int64_t i = at; i < g.h; i += ALONG) q[i] = finite && a > 0.0f ? nearest_small(to_f32(x[i]), a) : int8_t(0);
+    for (int64_t i = at; i < g.h; i += ALONG) q[i] = finite && a > 0.0f ? nearest_divided(to_f32(x[i]), a) : int8_t(0);
     return;
   }
   const float r = 127.0f / a;
