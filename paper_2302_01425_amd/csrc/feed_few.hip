@@ -194,8 +194,8 @@ __global__ __launch_bounds__(kFewThreads) void feed_few_kernel(FeedArgs g, int t
         v[o] = float(sum);
       }
       if constexpr (sizeof(T) == 1) {
-        v[0] = v[0] * scale * first_scale;
-        if constexpr (kOf == 2) v[1] = v[1] * scale * second_scale;
+        v[0] = scaled(v[0], row_scale(scale), first_scale);
+        if constexpr (kOf == 2) v[1] = scaled(v[1], row_scale(scale), second_scale);
       }
       if constexpr (WORK == kPlain) few_store<T, OUT, WORK, 0>(g, m, n, there, t, v[0], v[1]);
       else if (g.act == kSilu) few_store<T, OUT, WORK, kSilu>(g, m, n, there, t, v[0], v[1]);

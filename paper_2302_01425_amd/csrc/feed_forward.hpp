@@ -129,6 +129,20 @@ __device__ __forceinline__ float act_value(float g, float* slope) {
 }
 
 // ---- outputs --------------------------------------------------------------------------------------------------------------
+// A sum of 8-bit products with its scales, in an order in which nothing between leaves float32's range if the result does not: a row's
+// scale comes first where it is below 1 (a whole number times it keeps its digits, and the channel's may be large), the channel's where
+// it is not.  One of the two factors is 1.
+struct RowScale {
+  float first, last;
+};
+__device__ __forceinline__ RowScale row_scale(float scale) {
+  const bool small = scale < 1.0f;
+  return {small ? scale : 1.0f, small ? 1.0f : scale};
+}
+__device__ __forceinline__ float scaled(float sum, const RowScale& row, float channel) {
+  return sum * row.first * channel * row.last;
+}
+
 template <class T>
 __device__ __forceinline__ void load_four(const T* p, int64_t left, float (&v)[4]) {
   if (left >= 4) {
@@ -214,13 +228,14 @@ __device__ __forceinline__ void finish_tile(const ACC (&acc)[MI][NJ], const Feed
       const bool inside = m < m_end;
       OUT* row = static_cast<OUT*>(g.c) + m * g.c_stride;
       f32x16 first, second;
+      const RowScale scale = row_scale(rows.scale[i]);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int x = 4 * q + r;
           const auto of = [&](int at) {
-            return kEight ? float(acc[i][at][x]) * rows.scale[i] * col_scale[kEight ? at : 0][q][r] : float(acc[i][at][x]);
+            return kEight ? scaled(float(acc[i][at][x]), scale, col_scale[kEight ? at : 0][q][r]) : float(acc[i][at][x]);
           };
           first[x] = of(j);
           if constexpr (kOf == 2) second[x] = of(j + 1);

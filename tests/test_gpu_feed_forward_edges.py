@@ -1,8 +1,10 @@
-"""The experts' feed-forward on the GPU at its edges: rows in 8 bits up to the largest numbers."""
+"""The experts' feed-forward on the GPU at its edges: rows in 8 bits up to the largest numbers, scales of any size.  Comparisons and
+tolerances as in test_gpu_feed_forward.py."""
 import numpy as np
 import pytest
 
-from tests.test_gpu_experts import HALF, host, put, rounded
+from tests import test_gpu_feed_forward as base
+from tests.test_gpu_experts import HALF, TINY, U, host, put, rounded
 
 pytestmark = pytest.mark.gpu
 DTYPES = ("float32", "bfloat16", "float16")
@@ -46,3 +48,40 @@ def test_quantise_beside_halves_of_large_rows(gpu, h, dtype):
     q, scale = gpu.topk_quantise_rows(put(x, dtype))
     assert np.array_equal(host(q), want)
     assert np.array_equal(host(scale).astype(np.float32), a.astype(np.float32) / np.float32(127.0))
+
+
+# rows, k, n, h, f: by vector sums, 32 rows of half the columns and of all, 64 rows, 128 x 128, 256 x 256
+SCALED = [(1, 2, 4, 64, 40), (2, 2, 4, 4100, 24), (256, 2, 8, 512, 448), (300, 2, 2, 129, 1141), (2600, 2, 4, 264, 520),
+          (3000, 2, 8, 1040, 2176), (20, 2, 3, 9, 15)]
+
+
+@pytest.mark.parametrize("rows,k,n,h,f", SCALED)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_scales_of_any_size_in_8_bits(gpu, rows, k, n, h, f, dtype):
+    """Scales of rows and channels whose product is moderate, while either is near one end of float32: nothing between may leave its
+    range.  Two products and the sum's conversion are rounded: (HALF + 4 u) of the exact value; for the gated block three of either
+    sum and their product: (HALF + 8 u)."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(rows + h)
+    dt = getattr(torch, dtype)
+    source, offset, at = base.large_lists(gpu, rows, k, n, g)
+    q, wg, wu = (torch.randint(-128, 128, s, generator=g, device="cuda", dtype=torch.int8) for s in ((rows, h), (n, f, h), (n, f, h)))
+
+    def scale(shape, power):
+        return (torch.rand(shape, generator=g, device="cuda") + 1.0) * 2.0 ** power
+
+    for rows_power, channels_power in ((110, -126), (122, -138), (-126, 110), (-134, 118), (28, -44), (-44, 28)):
+        xs, gs, us = scale((rows,), rows_power), scale((n, f), channels_power), scale((n, f), channels_power)
+        xs[::5] *= 2.0 ** -3
+        xs[1::5] = 0.0                                      # (a row of zeros)
+        print("case", rows, k, n, h, f, dtype, rows_power, flush=True)
+        out = gpu.topk_expert_product_i8_fwd(q, xs, wg, gs, offset, source, k, dt)
+        both = gpu.topk_expert_gated_i8_fwd(q, xs, wg, gs, wu, us, offset, source, k, gpu.TOPK_ACT_RELU, dt)
+        for e in range(n):
+            part = slice(at[e], at[e + 1])
+            row = (source[part] // k).long()
+            xe = q[row].double()
+            a, b = ((xe @ w[e].double().t().contiguous()) * xs[row].double()[:, None] * s[e].double() for w, s in ((wg, gs), (wu, us)))
+            c = a.clamp(min=0) * b
+            assert (out[part].double() - a).abs().le((HALF[dtype] + 4 * U) * a.abs() + TINY[dtype]).all(), e
+            assert (both[part].double() - c).abs().le((HALF[dtype] + 8 * U) * c.abs() + TINY[dtype]).all(), e
