@@ -6,8 +6,9 @@
 // every CW-th column.  In 16 bits the instruction wants eight k of a column in a lane: eight such loads, put together by register halves.
 //
 // Bound by the time from a load to its use where experts are few, by HBM where they are many: one expert of 1 to 64 places, 2048 -> 1024,
-// gated, turned weights: float32 24 us (tiles of 64 rows through LDS 93), bfloat16 18 to 20 (24); 32 experts of 8, float32: 104 us, 5.1
-// TB/s of W (165).
+// gated, turned weights: float32 25 us (tiles of 64 rows through LDS 93), bfloat16 18 to 20 (24); 32 experts of 8, float32: 106 us, 5.1
+// TB/s of W (165).  float32 sums in one chain per wavefront took 24 and 106 us, with errors (root mean
+// square, of that of the sums, random terms) of 5.7e-7 at 4096 k and 1.13e-6 at 16384, where parts of 128 k have 2.1e-7 and 2.3e-7.
 #pragma once
 
 #include "feed_forward.hpp"
@@ -42,8 +43,19 @@ __global__ __launch_bounds__(kAcrossThreads, 2) void feed_across_kernel(FeedArgs
 
   Packed<T, N> va[kSets];
   Packed<T, CW> vb[kSets][N];
-  f32x16 sum[1][CW];
+  // (float32: sums of 128 k of the wavefront are added to the others' as a whole, as in feed_tiles.hpp.  Such an addition between the
+  // instructions of a step measured 10 % more, a loop of 128 k spilled.)
+  constexpr bool kApart = sizeof(T) == 4;
+  constexpr int kPartSteps = 128 / kStepK;
+  f32x16 sum[1][CW], part[1][CW];
+  f32x16(&to)[1][CW] = kApart ? part : sum;
   clear(sum);
+  clear(part);
+  const auto add_part = [&]() {
+#pragma unroll
+    for (int i = 0; i < CW; ++i) sum[0][i] += part[0][i];
+    clear(part);
+  };
   // N of k from `k` on, per half
   const auto load = [&](int set, int64_t k) {
     va[set] = load_packed<T, N>(reinterpret_cast<const T*>(a) + k);
@@ -59,7 +71,7 @@ __global__ __launch_bounds__(kAcrossThreads, 2) void feed_across_kernel(FeedArgs
 #pragma unroll
       for (int e = 0; e < N; ++e) fb[e] = vb[set][e].v[i];
 #pragma unroll
-      for (int q = 0; q < kMma<T>; ++q) sum[0][i] = mma(q, fb, fa, sum[0][i]);
+      for (int q = 0; q < kMma<T>; ++q) to[0][i] = mma(q, fb, fa, to[0][i]);
     }
   };
   const int64_t whole = g.depth / kStepK;
@@ -79,6 +91,7 @@ __global__ __launch_bounds__(kAcrossThreads, 2) void feed_across_kernel(FeedArgs
           load(set, k_of(i + kSets + set));
           __builtin_amdgcn_sched_barrier(0);
         }
+        if (kApart && (i + kSets) % kPartSteps == 0) add_part();
       }
 #pragma unroll
       for (int set = 0; set < kSets - 1; ++set)
@@ -97,6 +110,7 @@ __global__ __launch_bounds__(kAcrossThreads, 2) void feed_across_kernel(FeedArgs
       }
       multiply(0);
     }
+    if constexpr (kApart) add_part();
     a += g.a_apart, b += g.apart;
   }
 #pragma unroll

@@ -76,7 +76,16 @@ __global__ __launch_bounds__(kThinThreads) void feed_thin_kernel(FeedArgs g) {
 
   const auto rows = rows_of_tile<T, 1>(g, f.begin, f.end);
   Fragment<T> va[kThinSets][kParts][kA], vb[kThinSets][kParts][kB];
-  std::conditional_t<sizeof(T) == 1, i32x4, f32x4> sum[kA][kB] = {};
+  // (float32: sums of kThinSets steps, 96 k of the wavefront, are added to the others' as a whole, as in feed_tiles.hpp)
+  constexpr bool kApart = sizeof(T) == 4;
+  std::conditional_t<sizeof(T) == 1, i32x4, f32x4> sum[kA][kB] = {}, part[kA][kB] = {};
+  auto& to = kApart ? part : sum;
+  const auto add_part = [&]() {
+#pragma unroll
+    for (int i = 0; i < kA; ++i)
+#pragma unroll
+      for (int j = 0; j < kB; ++j) sum[i][j] += part[i][j], part[i][j] = {};
+  };
   const auto load = [&](int set, int64_t k0) {
 #pragma unroll
     for (int t = 0; t < kParts; ++t) {
@@ -94,7 +103,7 @@ __global__ __launch_bounds__(kThinThreads) void feed_thin_kernel(FeedArgs g) {
 #pragma unroll
         for (int i = 0; i < kA; ++i)
 #pragma unroll
-          for (int j = 0; j < kB; ++j) sum[i][j] = mma16(q, vb[set][t][j], va[set][t][i], sum[i][j]);
+          for (int j = 0; j < kB; ++j) to[i][j] = mma16(q, vb[set][t][j], va[set][t][i], to[i][j]);
   };
   // whole steps: step wave + 4 i is the wavefront's i-th, and those behind its last are read from there (without branches, so that
   // the waits count the loads of later steps out)
@@ -111,6 +120,7 @@ __global__ __launch_bounds__(kThinThreads) void feed_thin_kernel(FeedArgs g) {
         load(s, k_of(i + kThinSets + s));
         __builtin_amdgcn_sched_barrier(0);
       }
+      if constexpr (kApart) add_part();
     }
 #pragma unroll
     for (int s = 0; s < kThinSets - 1; ++s)
@@ -133,6 +143,7 @@ __global__ __launch_bounds__(kThinThreads) void feed_thin_kernel(FeedArgs g) {
     }
     multiply(0);
   }
+  if constexpr (kApart) add_part();
 #pragma unroll
   for (int i = 0; i < kA; ++i)
 #pragma unroll

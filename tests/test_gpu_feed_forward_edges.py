@@ -1,5 +1,5 @@
-"""The experts' feed-forward on the GPU at its edges: rows in 8 bits up to the largest numbers, scales of any size.  Comparisons and
-tolerances as in test_gpu_feed_forward.py."""
+"""The experts' feed-forward on the GPU at its edges: rows in 8 bits up to the largest numbers, scales of any size, long float32 sums.
+Comparisons and tolerances as in test_gpu_feed_forward.py."""
 import numpy as np
 import pytest
 
@@ -85,3 +85,56 @@ def test_scales_of_any_size_in_8_bits(gpu, rows, k, n, h, f, dtype):
             c = a.clamp(min=0) * b
             assert (out[part].double() - a).abs().le((HALF[dtype] + 4 * U) * a.abs() + TINY[dtype]).all(), e
             assert (both[part].double() - c).abs().le((HALF[dtype] + 8 * U) * c.abs() + TINY[dtype]).all(), e
+
+
+# ---- float32 sums -----------------------------------------------------------------------------------------------------
+
+# rows and columns: four rows at a time; 32 rows of half the columns, of all; 64 rows
+LONG = [(4, 64), (64, 64), (256, 768), (256, 1088), (1024, 1024)]
+
+
+def long_rows(m, h, big, seed):
+    """Ones, and 2^27 at `big`: additions of the others to it lose them, at most 8 each.  A part of 128 terms and the additions of at
+    most h / 128 parts and of a few wavefronts' sums are hence off by 128 + 8 (h / 128 + 8)."""
+    import torch
+    x = torch.ones((m, h), device="cuda")
+    x[:, big] = 2.0 ** 27
+    return x, 2.0 ** 27 + h - 1, 128 + 8 * (h // 128 + 8)
+
+
+@pytest.mark.parametrize("rows,f", LONG)
+@pytest.mark.parametrize("big", [0, 4100, 16383])
+def test_long_sums_of_float32(gpu, rows, f, big):
+    """max(g, 0) u with u = 1: g a sum of 16384 terms, W contiguous in k and with one row per k."""
+    import torch
+    h = 16384
+    x, want, most = long_rows(rows, h, big, 0)
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    wg, wu = torch.ones((1, f, h), device="cuda"), torch.zeros((1, f, h), device="cuda")
+    wu[:, :, 7] = 1.0
+    for turned in (False, True):
+        if turned:
+            wg, wu = (w.transpose(1, 2).contiguous().transpose(1, 2) for w in (wg, wu))
+        print("case", rows, f, big, turned, flush=True)
+        out = gpu.topk_expert_gated_fwd(x, wg, wu, off, act=gpu.TOPK_ACT_RELU)
+        off_by = float((out.double() - want).abs().max())
+        assert off_by <= most, (off_by, most)
+
+
+@pytest.mark.parametrize("rows,h", [(1, 64), (32, 64), (256, 2176), (1024, 2048)])
+@pytest.mark.parametrize("big", [0, 4100, 16383])
+def test_long_sums_of_float32_in_dx(gpu, rows, h, big):
+    """Kept sums of 1: dg = t, times ones."""
+    import torch
+    f = 16384
+    t, want, most = long_rows(rows, f, big, 0)
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    x, pre = torch.ones((rows, h), device="cuda"), torch.ones((rows, 2, f), device="cuda")
+    wg, wu = torch.ones((1, f, h), device="cuda"), torch.zeros((1, f, h), device="cuda")
+    for turned in (False, True):
+        if turned:
+            wg, wu = (w.transpose(1, 2).contiguous().transpose(1, 2) for w in (wg, wu))
+        print("case", rows, h, big, turned, flush=True)
+        dx = gpu.topk_expert_gated_vjp(x, wg, wu, off, t, act=gpu.TOPK_ACT_RELU, pre=pre, want_w=False)[0]
+        off_by = float((dx.double() - want).abs().max())
+        assert off_by <= most, (off_by, most)
