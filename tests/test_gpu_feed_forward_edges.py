@@ -1,5 +1,5 @@
-"""The experts' feed-forward on the GPU at its edges: rows in 8 bits up to the largest numbers, scales of any size, long float32 sums.
-Comparisons and tolerances as in test_gpu_feed_forward.py."""
+"""The experts' feed-forward on the GPU where test_gpu_feed_forward.py does not reach: rows in 8 bits up to the largest numbers, scales
+of any size, long float32 sums, and the kernels that only calls of certain sizes take.  Comparisons and tolerances as there."""
 import numpy as np
 import pytest
 
@@ -138,3 +138,36 @@ def test_long_sums_of_float32_in_dx(gpu, rows, h, big):
         dx = gpu.topk_expert_gated_vjp(x, wg, wu, off, t, act=gpu.TOPK_ACT_RELU, pre=pre, want_w=False)[0]
         off_by = float((dx.double() - want).abs().max())
         assert off_by <= most, (off_by, most)
+
+
+# ---- kernels that only some sizes take ----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows,k,n,h,f", [(8192, 2, 8, 1032, 1544), (8192, 2, 8, 1536, 1536)])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_dx_of_large_tiles(gpu, rows, k, n, h, f, dtype):
+    """dx by tiles of 256 x 256 (192 of them at least): several tiles of columns, whose sums begin at different steps, a last step and a
+    last tile that are not whole, and whole ones; weights contiguous in either direction."""
+    base.test_large_whole_numbers(gpu, rows, k, n, h, f, dtype)
+
+
+@pytest.mark.parametrize("rows,k,n,h,f", [(3000, 2, 8, 1040, 2176), (2100, 2, 6, 2064, 2048), (256, 2, 8, 512, 896), (256, 2, 8, 512, 448)])
+def test_8_bits_by_size(gpu, rows, k, n, h, f):
+    """256 x 256 with a last step that is not whole; 32 rows of all columns, plain (f 896) and gated (448)."""
+    base.test_large_products_of_8_bits(gpu, rows, k, n, h, f)
+
+
+@pytest.mark.parametrize("rows,k,n,h,f", [(8, 2, 4, 4096, 1024), (8, 2, 4, 4096, 512)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_few_rows_of_8_bits_in_turns(gpu, rows, k, n, h, f, dtype):
+    """k shared by wavefronts that take two turns of columns, plain (f 1024) and gated (512)."""
+    base.test_products_of_8_bits(gpu, rows, k, n, h, f, dtype)
+
+
+@pytest.mark.parametrize("rows,k,n,h,f,dtype", [(1, 2, 8, 2048, 1024, "bfloat16"), (1, 2, 8, 2048, 1024, "float16"),
+                                                (1, 2, 2, 2049, 2201, "bfloat16"), (1, 2, 2, 2049, 2201, "float16"),
+                                                (4, 2, 4, 1100, 1501, "float32"), (4, 2, 4, 1027, 702, "float32"),
+                                                (256, 2, 8, 2049, 150, "bfloat16"), (256, 2, 8, 2049, 150, "float16")])
+def test_few_rows_by_size(gpu, rows, k, n, h, f, dtype):
+    """k shared by the wavefronts in 16 bits, in one and two turns of columns; in float32 in four and two; 32 rows of half the columns
+    where W's rows begin anywhere."""
+    base.test_whole_numbers(gpu, rows, k, n, h, f, dtype)
