@@ -36,16 +36,25 @@ bool whole_parts(const void* p, int64_t stride, int64_t length, int size) {
 //     / 104 / 69, 1 x 128 4096 -> 4096 299 / 70 / 54 / 57, 2 x 128 564 / 135 / 102 / 62.
 //     Rows of W that do not begin at 16 bytes, 1001 -> 300: 8 x 4 7.8 / 14.4 / 21 / 19, 8 x 32 20 / 17.4 / 24 / 18.4, 32 x 4 15.4 /
 //     33 / 36 / 23.
-//     float32: 1 x 1 2048 -> 1024 7.1 / 14.9 / 25 / 95, 1 x 32 22 / 21 / 29 / 95, 8 x 32 144 / 47 / 45 / 108, 32 x 32 549 / 164 / 141 /
-//     196, 8 x 128 444 / 136 / 116 / 110, 8 x 1 4096 -> 4096 192 / 239 / 233 / 348, 8 x 128 1001 -> 300 62 / 28 / 35 / 55.
+//     16 bits, 32 rows of all / 64 rows by tiles of 32 rows: 512, places 8 to 32 per expert 31 to 34 / 36 to 38, 64 30 / 30; 640, 64 places
+//     42 / 32, 32 places 47 / 46; 768, 8 to 32 places 43 to 48 / 45; 1024, 16 60 / 67, 32 63 / 61.
+//     float32: 1 x 1 2048 -> 1024 7.1 / 15.4 / 24 / 96, 1 x 32 17 / 21 / 30 / 95, 8 x 32 114 / 43 / 39 / 107, 32 x 32 426 / 155 / 138 /
+//     170, 8 x 128 - / 137 / 114 / 109, 8 x 1 4096 -> 4096 182 / 210 / 212 / 319.  64 rows at a time are half empty where experts have 32
+//     places or fewer, and take a whole round of 512 workgroups each time.  By tiles of 32 rows, narrow / thin / small: 768, 64 places
+//     109 / 93 / 110, 128 102 / 86 / 105, 512 -> 1024 39 / 35 / 31; 832, 64 places 124 / 118 / 111; 896, 128 119 / 112 / 106; 1152, 64
+//     158 / 146 / 164; 2048, 64 274 / 230 / 180; 1152, 32 places 177 / 166 / 260; 2048, 32 305 / 262 / 334; 4096, 32 619 / 528 / 667,
+//     8 443 / 433 / 646.  Rows of W that begin anywhere, 8 x 128 1001 -> 300 (320 tiles) 27 / 35 / 54, 1001 -> 1001: 384, 8 places 35 / 38
+//     / 60, 32 43 / 42 / 59; 512, 8 44 / 40 / 62, 32 58 / 46 / 63, 128 42 / 36 / 55; 768, 64 64 / 64 / 60; 1024, 64 84 / 74 / 63, 32 106
+//     / 91 / 95; 2048, 32 193 / 171 / 185.
 //     8 bits, plain: 1 x 8 2048 -> 1024 4.8 / 7.7 / 10.9 / 12.7, 1 x 64 10.2 / 9.3 / 12.7 / 12.1, 8 x 64 39 / 14.9 / 13.3 / 13.5, 32 x 8
 //     24 / 21 / 20 / 16.5, 8 x 8 512 -> 512 6.4 / 5.2 / 6.8 / 6.7; gated: 1 x 8 5.5 / 8.4 / 11.1 / 14.9, 8 x 32 40 / 15.8 / 13.0 / 16.7,
 //     32 x 8 46 / 40 / 35 / 26.
-//   W with one row per k, 32 rows of half the columns / of all / 64 rows (us, turned weights; dx of kept sums): float32 1 x 1 2048 -> 1024
-//     24 / 39 / 94; 26 / 40 / 68, 8 x 32 41 / 47 / 104; 46 / 51 / 82, 8 x 64 (256 tiles of all) 68 / 47 / 104; 66 / 52 / 84, 32 x 8 117 /
-//     104 / 165; 126 / 108 / 189, 32 x 64 (1024) 241 / 177 / 177; 236 / 188 / 211, 8 x 250 1000 -> 1500 (1536; 512) 164 / 134 / 132; 162 /
-//     140 / 163.  bfloat16 1 x 1 2048 -> 1024 18.3 / 32 / 24; 19.8 / 33 / 24, 8 x 1 (128) 28.7 / 49 / 33; 29.4 / 49 / 31, 8 x 64 43 / 50 / 36;
-//     37 / 50 / 33, 8 x 32 1001 -> 301 15 / 22 / 18; 12.6 / 18 / 14.
+//   W with one row per k, 32 rows of half the columns / of all / 64 rows (us, turned weights; dx of kept sums with its slopes, tiles of 32
+//     rows of all columns in brackets): float32 1 x 1 2048 -> 1024 25 / 40 / 93; 26 / 41 / 67, 8 x 32 (128) 41 / 47 / 103; 43 / 49 / 79,
+//     8 x 64 (256) 67 / 48 / 104; 62 / 50 / 81, 32 x 8 (512) 121 / 106 / 166; 111 / 104 / 183, 32 x 64 (1024) 235 / 177 / 179; 227 / 178 /
+//     203.  1024 -> 1024, 128 x 8 (2048; 1024) 224 / 206 / 333; 215 / 217 / 351, 128 x 32 298 / 238 / 341; 305 / 265 / 369, 64 x 64 236 / 178 /
+//     184; 236 / 194 / 206, 16 x 256 205 / 160 / 165.  bfloat16 1 x 1 2048 -> 1024 18.3 / 32 / 24; 19.8 / 33 / 24, 8 x 1 (128) 28.7 / 49 / 33;
+//     29.4 / 49 / 31, 8 x 64 43 / 50 / 36; 37 / 50 / 33, 8 x 32 1001 -> 301 15 / 22 / 18; 12.6 / 18 / 14.
 //   whole parts, 128 x 128 / 256 x 256: 8 x 250 1000 -> 1500 (96 tiles) 33 / 37, 24 x 125 1024 -> 768 (144) 29 / 33, 5 x 1925 640 ->
 //     1088 (360) 58 / 52, 32 x 512 2048 -> 2048 (1024) 427 / 310.
 template <class T>
@@ -64,17 +73,17 @@ int launch_feed(const FeedArgs& g, bool k_contiguous, Work work, hipStream_t str
                    : s == 2 ? multiplied <= (aligned ? 1 << 25 : 100000000)
                             : multiplied <= 100000000 || share <= 4;
     if (few) return launch_feed_few<T>(g, work, stream);
-    if (tiles < (s == 2 && !aligned ? 96 : 192) || (s == 4 && !aligned && tiles < 1024))
-      return launch_feed_thin<T>(g, work, true, stream);
-    const bool thin = s == 1 ? tiles < 300 : s == 2 ? tiles < 768 || (tiles <= 1024 && share <= 16)
-                                                    : tiles < 1024 || (tiles == 1024 && share <= 32);
-    if (aligned && thin) return launch_feed_thin<T>(g, work, false, stream);
+    if (tiles < (aligned ? 192 : s == 2 ? 96 : s == 4 ? 448 : 192)) return launch_feed_thin<T>(g, work, true, stream);
+    const bool thin = s == 1 ? tiles < 300
+                    : s == 2 ? tiles <= (share <= 16 ? 1024 : share <= 32 ? 768 : 512)
+                             : tiles <= 768 || share <= 32;
+    if ((aligned || s == 4) && thin) return launch_feed_thin<T>(g, work, false, stream);
   }
   if constexpr (s > 1) {
     const int64_t tiles = experts * cut(share, 32) * cut(g.cols, pair ? 64 : 128);
     const bool narrow = s == 2 || tiles <= 128;
     if (!k_contiguous && g.limit > 0 && g.depth * s >= 16 && g.cols >= (pair ? 64 : 128) / (narrow ? 2 : 1) &&
-        tiles <= (s == 4 ? 1024 : 128) && (g.slots / 4 + g.n) * cut(g.cols, 2) < most)
+        (tiles <= (s == 4 ? 1024 : 128) || (s == 4 && share <= 32)) && (g.slots / 4 + g.n) * cut(g.cols, 2) < most)
       return launch_feed_across<T>(g, work, narrow, stream);
   }
   if constexpr (s < 4) {

@@ -171,3 +171,11 @@ def test_few_rows_by_size(gpu, rows, k, n, h, f, dtype):
     """k shared by the wavefronts in 16 bits, in one and two turns of columns; in float32 in four and two; 32 rows of half the columns
     where W's rows begin anywhere."""
     base.test_whole_numbers(gpu, rows, k, n, h, f, dtype)
+
+
+@pytest.mark.parametrize("rows,k,n,h,f", [(130, 2, 16, 1001, 1001), (400, 2, 40, 520, 2048), (300, 2, 12, 776, 1032)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_many_experts_of_few_rows(gpu, rows, k, n, h, f, dtype):
+    """32 rows of all columns: float32 at any alignment (512 tiles), more than 1024 tiles of experts with at most 32 places, also where W
+    has one row per k; 50 places per expert (792 tiles: 64 rows)."""
+    base.test_large_whole_numbers(gpu, rows, k, n, h, f, dtype)
