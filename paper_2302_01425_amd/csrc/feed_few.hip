@@ -172,8 +172,8 @@ __global__ __launch_bounds__(kFewThreads) void feed_few_kernel(FeedArgs g, int t
     }
     Sum acc[kFewCols * kFewRows] = {};
     constexpr int64_t kStride = (SHARED ? kFewWaves : 1) * kChunk;
-    // (one copy of the instructions, which are read from memory by every launch: with two steps at a time and the last by itself one
-    // token of 2048 -> 1024 took 10.5 us in the place of 9.0)
+    // (one copy of the instructions, which are read from memory by every launch: with two steps at a time and the last by itself a call
+    // of one token, 2048 -> 1024, took 10.2 us in the place of 8.5)
 #pragma unroll 1
     for (int64_t k = (SHARED ? wave * kChunk : 0) + lane * N; k < g.depth; k += kStride) {
       const int64_t from = min(k, g.depth - N);

@@ -223,6 +223,7 @@ int launch_gated_vjp(int type, const GatedArgs& g, hipStream_t stream) {
     const int64_t tiles = both_weights_tiles(w);
     const bool whole = s == 2 && p.m > 0 && whole_parts(w.a, w.a_stride, w.m, s) && whole_parts(w.b, w.b_stride, w.cols, s);
     // (one launch, of a few more workgroups than tiles; products of rows and strides in 32 bits)
+    // (they cross between 1024 and 1536 places, times beside the kernel)
     if (whole && tiles >= 256 && tiles < (int64_t(1) << 22) && w.a_stride < (int64_t(1) << 31) && w.b_stride < (int64_t(1) << 31) &&
         even_share(p.slots, p.n) >= 1536)
       return launch_both_weights(type, w, x_first, apart, p.dw, g.dw_up, stream);

@@ -93,7 +93,7 @@ __device__ __forceinline__ float inverse(float x) {
 //   silu       g p, p = 1 / (1 + exp(-g));  p + g p (1 - p)
 //   gelu       g F, F = P(N(0, 1) < g);  F + g exp(-g^2 / 2) / sqrt(2 pi).  F(-|g|) = exp(-g^2 / 2) q(t) t, t = 1 / (1 + 0.4 |g| /
 //              sqrt 2), with q the polynomial of degree 10 through the Chebyshev nodes of t in (0, 1) of exp(x^2) erfc(x) / 2 t, x =
-//              (1 / t - 1) / 0.4: off by 8e-9 of it, 3.2e-7 in float32.  g^2 is taken with the rounding it lost.
+//              (1 / t - 1) / 0.4: off by 1.5e-8 of it with these coefficients, 3.4e-7 in float32.  g^2 is taken with the rounding it lost.
 //   gelu_tanh  g (1 + tanh z) / 2 = g p(2 z), z = sqrt(2 / pi) (g + 0.044715 g^3)
 //   relu       g where g > 0, slope 0 at 0
 // NaN gives NaN (relu: and the slope 1).

@@ -6,9 +6,12 @@
 // one array, every die an eighth of every expert's (split_tiles).  Slopes of a place without a row of x are zeros; its row of x,
 // and what lies behind an expert's last place, is read as zeros.
 //
-// Half as many operand bytes per output as tiles of 128 x 256, but nothing overlaps a tile's stores, so for experts of many places: both
-// weights of 8192 x 4096 from 8192 places 865 us (1.27 PFLOP/s), with the other tiles, a launch per weight, 1028; 32 experts of 512
-// places, 2048 x 2048, 490 and 455 (390 with the others' in one launch).
+// Two thirds of the operand bytes per output of tiles of 128 x 256 (expert_product_tiles.hip, both weights in one launch too), but nothing
+// overlaps a tile's stores, so for experts of many places.  Slopes of kept sums and both weights, bfloat16, these / those, rows in expert
+// order; found through source: 2048 x 2048, 32 experts of 512 places 484 / 432 us; 509 / 449, 16 of 1024 375 / 355; 395 / 388, 12 of 1280 330
+// / 323; 347 / 348, 10 of 1536 315 / 310; 331 / 338, 8 of 2048 317 / 322; 335 / 350, 2 of 8192 271 / 295; 287 / 323.  1024 x 1024, 16 of 1024
+// 103 / 101; 108 / 111, of 1536 144 / 150; 151 / 162.  4096 x 4096, one of 512 55 / 53; 58 / 58, of 1024 80 / 81; 87 / 92, of 2048 134 /
+// 144; 145 / 161.  8192 x 4096 from 8192 places 877 / 1015; 963 / 1120.  The weights alone: 865 us, 1.27 PFLOP/s.
 #include "feed_forward.hpp"
 
 namespace topk {
