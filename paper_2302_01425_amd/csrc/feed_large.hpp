@@ -7,9 +7,9 @@
 // 32 bytes of k are read while those of the 32 before are multiplied, and loads are issued one by one between the instructions.
 //
 // Bound by the matrix instructions and the clock they leave where k is long (8192 rows, 8192 -> 4096, gated: bfloat16 830 to 954 us,
-// 1.15 to 1.32 PFLOP/s; 8 bits 472 us, 2.33 POP/s), by 8 to 9 us of start and end per tile where it is not (8192 x 2 places, 32
-// experts, 2048 -> 2048, gated: 310 to 326 us, 0.84 to 0.89 PFLOP/s, matrix units busy 42 %; slopes 364; dx 313; 8 bits 196, plain to 4096
-// 203).  Steps of 64 bytes read half lines and measured slower; tiles that a workgroup takes one after the other spilled.
+// 1.15 to 1.32 PFLOP/s; 8 bits 458 to 472 us, 2.33 to 2.40 POP/s), by 8 to 9 us of start and end per tile where it is not (8192 x 2 places, 32
+// experts, 2048 -> 2048, gated: 310 to 327 us, 0.84 to 0.89 PFLOP/s, matrix units busy 42 %; slopes 364; dx 313; 8 bits 200, plain to 4096
+// 207).  Steps of 64 bytes read half lines and measured slower; tiles that a workgroup takes one after the other spilled.
 #pragma once
 
 #include "feed_forward.hpp"
