@@ -130,13 +130,13 @@ __device__ __forceinline__ float act_value(float g, float* slope) {
 
 // ---- outputs --------------------------------------------------------------------------------------------------------------
 // A sum of 8-bit products with its scales, in an order in which nothing between leaves float32's range if the result does not: a row's
-// scale comes first where it is below 1 (a whole number times it keeps its digits, and the channel's may be large), the channel's where
+// scale comes first where its magnitude is below 1 (a whole number times it keeps its digits, and the channel's may be large), the channel's where
 // it is not.  One of the two factors is 1.
 struct RowScale {
   float first, last;
 };
 __device__ __forceinline__ RowScale row_scale(float scale) {
-  const bool small = scale < 1.0f;
+  const bool small = fabsf(scale) < 1.0f;
   return {small ? scale : 1.0f, small ? 1.0f : scale};
 }
 __device__ __forceinline__ float scaled(float sum, const RowScale& row, float channel) {

@@ -74,6 +74,8 @@ def test_scales_of_any_size_in_8_bits(gpu, rows, k, n, h, f, dtype):
         xs, gs, us = scale((rows,), rows_power), scale((n, f), channels_power), scale((n, f), channels_power)
         xs[::5] *= 2.0 ** -3
         xs[1::5] = 0.0                                      # (a row of zeros)
+        xs[2::5] *= -1.0
+        gs[:, ::3] *= -1.0
         print("case", rows, k, n, h, f, dtype, rows_power, flush=True)
         out = gpu.topk_expert_product_i8_fwd(q, xs, wg, gs, offset, source, k, dt)
         both = gpu.topk_expert_gated_i8_fwd(q, xs, wg, gs, wu, us, offset, source, k, gpu.TOPK_ACT_RELU, dt)
